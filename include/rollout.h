@@ -238,6 +238,141 @@ rl_status rl_gae(const float* reward, const uint8_t* done, const float* value, c
                  int32_t n_steps, int32_t n_envs, int32_t n_agents, float gamma, float lambda, float* adv,
                  float* ret, void* stream);
 
+/* ---- a learner's operators: the recurrence over a stored trajectory, its
+ * gradient, the policy loss and the orthogonalised update ----
+ *
+ * Rows of a trajectory are the agents of its envs, step-major as rollout_run*
+ * write them: [T, E, A, ..].  Floating inputs may hold any value; a NaN or
+ * infinity stays in the row and channel (rl_scan*), row (rl_ppo_loss; the
+ * stats and, with normalize_adv, advantages are shared by all rows) or matrix
+ * (rl_orthogonalize) that holds it.  Outputs must not overlap inputs or one
+ * another except where a pair is allowed below (RL_EINVAL otherwise).  A
+ * call's workspace is device memory owned by the caller, 16-byte aligned, not
+ * read across calls; two calls that may overlap in time need one each, and so
+ * do two captured graphs that may. */
+
+/* Linear recurrence over a trajectory, for every agent and channel:
+ *   h_t = a_t k_t h_{t-1} + u_t,  t = 0 .. T-1,   h_last = k_T h_{T-1},
+ * with h_{-1} = h0, k_0 = 1 and, for t >= 1, k_t = 0 where done[t-1] != 0 and 1
+ * otherwise: a state does not outlive its episode, as in rollout_run_s5, and
+ * h_last is what the next call's h0 has to be.  Where k_t = 0, h_t is u_t
+ * exactly (neither the gate nor the old state is read into it).
+ *   RL_SCAN_GATED     a_t [T, E, A, D], a gate for every step and channel (a
+ *                     gated linear recurrence), of the values' dtype.
+ *   RL_SCAN_DIAGONAL  a = lambda_bar [2, P] float32, one complex factor per
+ *                     state channel, as rl_s5_discretize makes it; u, h and
+ *                     the states [.., 2, P] hold real, then imaginary parts
+ *                     (with u = B_bar of the encoder's outputs, h is the x_t
+ *                     of the S5 network below).
+ * T = 1 with h_last in h0's place is one step of a policy that acts.
+ * Values (u, gate, h and their gradients) are float32 or bfloat16; states
+ * (h0, h_last, dh0, dh_last), lambda_bar and its gradient are float32, and the
+ * recurrence runs in float32.  Long runs of few rows are cut into segments
+ * that are folded as affine maps, so T steps in one call and in two agree to
+ * rounding, not to the bit; gates are expected not to let the product of
+ * a segment's gates overflow float32 (|a| <= 1 never does).  Equal calls give equal
+ * bits.
+ * Limits: sizes >= 1; n_envs * n_agents * width (twice that for
+ * RL_SCAN_DIAGONAL) < 2^31. */
+enum { RL_SCAN_GATED = 0, RL_SCAN_DIAGONAL = 1 };
+typedef struct {
+  int32_t kind;     /* RL_SCAN_* */
+  int32_t dtype;    /* RL_F32 or RL_BF16: u, gate, h, dh, du, dgate */
+  int32_t n_steps;  /* T */
+  int32_t n_envs;   /* E */
+  int32_t n_agents; /* A */
+  int32_t width;    /* D channels, or P complex state channels */
+} rl_scan_config;
+
+/* Bytes of workspace rl_scan (backward == 0) or rl_scan_backward (backward
+ * != 0) needs; 0 when it needs none or the config is invalid. */
+size_t rl_scan_workspace_bytes(const rl_scan_config* cfg, int32_t backward);
+
+/*   u [T, E, A, D] or [T, E, A, 2, P] read; gate read (see above);
+ *   done [T, E] uint8 read, may be NULL (no episode ends);
+ *   h0 [E, A, D] or [E, A, 2, P] float32 read, may be NULL (zeros);
+ *   h like u, written, may be NULL; h_last like h0, written, may be NULL or
+ *   h0 itself (one of h and h_last is required). */
+rl_status rl_scan(const rl_scan_config* cfg, const void* u, const void* gate, const uint8_t* done, const float* h0,
+                  void* h, float* h_last, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of a loss through rl_scan, given dh = dL/dh_t and dh_last =
+ * dL/dh_last (complex values: derivatives by the real and by the imaginary
+ * parts):
+ *   g_t = dh_t + conj(a_{t+1}) k_{t+1} g_{t+1},  g_{T-1} = dh_{T-1} + k_T dh_last,
+ *   du_t = g_t,  dgate_t = g_t k_t h_{t-1} (RL_SCAN_DIAGONAL: the sum of
+ *   g_t conj(k_t h_{t-1}) over steps, envs and agents),  dh0 = conj(a_0) g_0.
+ *   gate, done, h0 as given to rl_scan; h as it wrote it; dh like h; dh_last
+ *   like h0, may be NULL (zeros); all read.
+ *   du like h, written; dgate like gate, written, may be NULL (then h and h0
+ *   are not read and may be NULL); dh0 like h0, written, may be NULL or
+ *   dh_last itself.
+ * The previous state in dgate is the stored h: with RL_BF16 its rounding to
+ * bfloat16 enters dgate. */
+rl_status rl_scan_backward(const rl_scan_config* cfg, const void* gate, const uint8_t* done, const float* h0,
+                           const void* h, const void* dh, const float* dh_last, void* du, void* dgate, float* dh0,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Proximal policy optimisation's loss over R stored rows (agents at steps)
+ * and its gradients by the logits and values.  With l the logits of the legal
+ * actions (legal != 0 and logit > -inf), p = softmax(l), a the row's action:
+ *   ratio r = exp(log p_a - logp_old),
+ *   policy  -min(r adv, clamp(r, 1 - clip, 1 + clip) adv),
+ *   value   0.5 (v - ret)^2; with value_clip > 0 the larger of that and
+ *           0.5 (v_old + clamp(v - v_old, -value_clip, value_clip) - ret)^2
+ *           (on equality the first one's gradient),
+ *   entropy -sum p log p,
+ *   loss = mean(policy) + value_coef mean(value) - entropy_coef mean(entropy),
+ * the means taken over the n rows whose mask is not 0 (mask NULL: all rows).
+ * With normalize_adv, adv is first replaced by (adv - mean) / (std + 1e-8)
+ * over those rows (the population's standard deviation, n in the
+ * denominator).  A row without a legal action (an agent that waits) adds
+ * nothing to policy and entropy, and neither does the policy term of a row
+ * whose action is illegal or outside 0..nA-1.  Rows with mask 0 give zero
+ * gradients and nothing else, whatever they hold; with n = 0 everything is 0.
+ * Whether r and v - v_old lie beyond their borders is decided as in
+ * float64. */
+typedef struct {
+  int64_t n_rows;        /* R >= 1 */
+  int32_t n_actions;     /* nA in 1..32 */
+  int32_t normalize_adv; /* 0 or 1 */
+  float clip;            /* > 0, finite */
+  float value_clip;      /* > 0 and finite, or 0: no clipped value loss */
+  float value_coef;      /* finite */
+  float entropy_coef;    /* finite */
+} rl_ppo_config;
+
+/* Bytes of workspace rl_ppo_loss needs; 0 if the config is invalid. */
+size_t rl_ppo_workspace_bytes(const rl_ppo_config* cfg);
+
+/*   logits [R, nA] float32, legal [R, nA] uint8 or NULL (all legal), mask [R]
+ *   uint8 or NULL, actions [R] int32, logp_old, adv, value, ret [R] float32,
+ *   value_old [R] float32 (may be NULL when value_clip is 0), all read;
+ *   dlogits [R, nA] float32 written (0 for illegal actions); dvalue [R]
+ *   float32 written; stats [6] float32 written: loss, mean policy, mean value,
+ *   mean entropy, mean of r - 1 - log r over rows with a policy term (an
+ *   estimate of the KL divergence; n in the denominator) and the fraction of
+ *   rows whose ratio lies outside 1 -+ clip. */
+rl_status rl_ppo_loss(const rl_ppo_config* cfg, const float* logits, const uint8_t* legal, const uint8_t* mask,
+                      const int32_t* actions, const float* logp_old, const float* adv, const float* value,
+                      const float* value_old, const float* ret, float* dlogits, float* dvalue, float* stats,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Orthogonalised weight updates (the Muon optimiser, Jordan et al., 2024):
+ * for each of n matrices G [rows, cols] (a layer of a Policy, or of the n
+ * policies of a population), X_0 = G / |G|_F (0 for a zero matrix) and `steps`
+ * times
+ *   X <- a X + (b A + c A A) X,  A = X X^T,   a, b, c = 3.4445, -4.7750, 2.0315
+ * (on X^T when rows > cols), which moves the singular values of G towards 1.
+ * Values are read and written in `dtype`; X is kept in float32, products are
+ * formed from operands split into pairs of float16 (22 mantissa bits) and
+ * accumulated in float32.
+ *   g [n, rows, cols] read; out like g, written, may be g itself.
+ * Limits: n in 1..65535, rows and cols in 1..16384, steps in 1..32. */
+size_t rl_orthogonalize_workspace_bytes(int32_t n, int32_t rows, int32_t cols, int32_t dtype);
+rl_status rl_orthogonalize(int32_t n, int32_t rows, int32_t cols, int32_t dtype, int32_t steps, const void* g,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The rollout of rollout_run with one policy per agent slot, drawn from a
  * population: the ego agent and its teammates of the ad hoc teamwork objective
  * (Section 3, the J_AHT equation: the ego policy paired with teammate

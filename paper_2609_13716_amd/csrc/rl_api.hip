@@ -1,9 +1,12 @@
 // C-ABI entry points: host-side validation, then one kernel launch on the
 // caller's stream.  No device memory is allocated and no call waits on the
 // device.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
+
+#include <initializer_list>
 
 #include "rollout.h"
 #include "rl_internal.h"
@@ -182,6 +185,97 @@ rl_status check_policy(const rl_policy* pol, rl::PolicyArgs* a) {
       a->Wp[l] = pol->packed ? static_cast<const uint8_t*>(pol->packed) + rl::packed_layer_offset(dims, l) : nullptr;
     }
   }
+  return RL_OK;
+}
+
+// ---- the learner's operators ----
+
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+
+bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || !a.bytes || !b.bytes) return false;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x < y + b.bytes && y < x + a.bytes;
+}
+
+// Whether an output overlaps an input or another output; (pin, pout) is the
+// one pair that may be the same array.
+template <size_t NI, size_t NO>
+bool aliased(const Span (&in)[NI], const Span (&out)[NO], const void* pin = nullptr, const void* pout = nullptr) {
+  for (size_t o = 0; o < NO; ++o) {
+    for (size_t i = 0; i < NI; ++i) {
+      const bool allowed = pout && pin == pout && out[o].p == pout && in[i].p == pin;
+      if (!allowed && overlap(in[i], out[o])) return true;
+    }
+    for (size_t q = 0; q < o; ++q)
+      if (overlap(out[q], out[o])) return true;
+  }
+  return false;
+}
+
+bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+rl_status check_scan(const rl_scan_config* cfg, rl::ScanArgs* a) {
+  if (!cfg) return fail(RL_EINVAL, "cfg is NULL");
+  if (cfg->kind != RL_SCAN_GATED && cfg->kind != RL_SCAN_DIAGONAL)
+    return fail(RL_EUNSUPPORTED, "scan kind %d is not known", cfg->kind);
+  if (!valid_dtype(cfg->dtype)) return fail(RL_EUNSUPPORTED, "scan dtype %d is not known", cfg->dtype);
+  if (cfg->n_steps < 1 || cfg->n_envs < 1 || cfg->n_agents < 1 || cfg->width < 1)
+    return fail(RL_EINVAL, "sizes must be >= 1");
+  const bool diag = cfg->kind == RL_SCAN_DIAGONAL;
+  const int64_t most = INT32_MAX;  // divided step by step: the product itself may pass 64 bits
+  if (cfg->n_agents > most / cfg->n_envs || cfg->width > most / ((int64_t)cfg->n_envs * cfg->n_agents * (diag ? 2 : 1)))
+    return fail(RL_EINVAL, "a step of %d envs x %d agents x %d channels has 2^31 values or more", cfg->n_envs,
+                cfg->n_agents, cfg->width);
+  *a = rl::ScanArgs{diag, cfg->dtype == RL_BF16 ? rl::DT_BF16 : rl::DT_F32, cfg->n_steps, cfg->n_envs, cfg->n_agents,
+                    cfg->width};
+  return RL_OK;
+}
+
+struct ScanBytes {
+  size_t values, gate, done, state;
+};
+
+ScanBytes scan_bytes(const rl::ScanArgs& a) {
+  const size_t state = (size_t)a.E * a.A * a.W * (a.diag ? 2 : 1);
+  const size_t values = state * a.T * (a.dt == rl::DT_BF16 ? 2 : 4);
+  return {values, a.diag ? (size_t)8 * a.W : values, (size_t)a.T * a.E, 4 * state};
+}
+
+// Values aligned to their elements, states (and lambda_bar) to floats.
+bool scan_aligned(const rl::ScanArgs& a, std::initializer_list<const void*> values,
+                  std::initializer_list<const void*> states, const void* gate) {
+  const size_t es = a.dt == rl::DT_BF16 ? 2 : 4;
+  for (const void* p : values)
+    if (!aligned_to(p, es)) return false;
+  for (const void* p : states)
+    if (!aligned_to(p, 4)) return false;
+  return aligned_to(gate, a.diag ? 4 : es);
+}
+
+rl_status check_ppo(const rl_ppo_config* cfg) {
+  if (!cfg) return fail(RL_EINVAL, "cfg is NULL");
+  if (cfg->n_rows < 1 || cfg->n_rows > ((int64_t)1 << 40)) return fail(RL_EINVAL, "n_rows outside 1..2^40");
+  if (cfg->n_actions < 1 || cfg->n_actions > rl::MAX_NA)
+    return fail(RL_EUNSUPPORTED, "n_actions %d outside 1..%d", cfg->n_actions, rl::MAX_NA);
+  if (cfg->normalize_adv != 0 && cfg->normalize_adv != 1) return fail(RL_EINVAL, "normalize_adv must be 0 or 1");
+  if (!(cfg->clip > 0.f) || !isfinite(cfg->clip)) return fail(RL_EINVAL, "clip must be > 0 and finite");
+  if (!(cfg->value_clip >= 0.f) || !isfinite(cfg->value_clip))
+    return fail(RL_EINVAL, "value_clip must be >= 0 and finite");
+  if (!isfinite(cfg->value_coef) || !isfinite(cfg->entropy_coef))
+    return fail(RL_EINVAL, "value_coef and entropy_coef must be finite");
+  return RL_OK;
+}
+
+rl_status check_ortho(const rl::OrthoArgs& a) {
+  if (!valid_dtype(a.dt)) return fail(RL_EUNSUPPORTED, "dtype %d is not known", a.dt);
+  if (a.n < 1 || a.n > 65535) return fail(RL_EINVAL, "n %d outside 1..65535", a.n);
+  if (a.rows < 1 || a.rows > 16384 || a.cols < 1 || a.cols > 16384)
+    return fail(RL_EINVAL, "a %d x %d matrix is outside 1..16384", a.rows, a.cols);
+  if (a.steps < 1 || a.steps > 32) return fail(RL_EINVAL, "steps %d outside 1..32", a.steps);
   return RL_OK;
 }
 
@@ -490,6 +584,109 @@ rl_status rl_gae(const float* reward, const uint8_t* done, const float* value, c
   return launched(rl::launch_gae(reward, done, value, value_last, n_steps, n_envs, n_agents, gamma, lambda, adv,
                                  ret, (hipStream_t)stream),
                   "rl_gae");
+}
+
+size_t rl_scan_workspace_bytes(const rl_scan_config* cfg, int32_t backward) {
+  rl::ScanArgs a;
+  if (check_scan(cfg, &a) != RL_OK) return 0;
+  ok();
+  return rl::scan_workspace_bytes(a, backward != 0);
+}
+
+rl_status rl_scan(const rl_scan_config* cfg, const void* u, const void* gate, const uint8_t* done, const float* h0,
+                  void* h, float* h_last, void* workspace, size_t workspace_bytes, void* stream) {
+  rl::ScanArgs a;
+  const rl_status s = check_scan(cfg, &a);
+  if (s != RL_OK) return s;
+  if (!u || !gate) return fail(RL_EINVAL, "a required pointer is NULL");
+  if (!h && !h_last) return fail(RL_EINVAL, "both h and h_last are NULL");
+  const ScanBytes b = scan_bytes(a);
+  const Span in[] = {{u, b.values}, {gate, b.gate}, {done, b.done}, {h0, b.state}};
+  const Span out[] = {{h, b.values}, {h_last, b.state}, {workspace, workspace_bytes}};
+  if (aliased(in, out, h0, h_last)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (!scan_aligned(a, {u, h}, {h0, h_last}, gate)) return fail(RL_EINVAL, "an array is not aligned to its elements");
+  const size_t need = rl::scan_workspace_bytes(a, false);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
+  return launched(rl::launch_scan(a, u, gate, done, h0, h, h_last, workspace, (hipStream_t)stream), "rl_scan");
+}
+
+rl_status rl_scan_backward(const rl_scan_config* cfg, const void* gate, const uint8_t* done, const float* h0,
+                           const void* h, const void* dh, const float* dh_last, void* du, void* dgate, float* dh0,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  rl::ScanArgs a;
+  const rl_status s = check_scan(cfg, &a);
+  if (s != RL_OK) return s;
+  if (!gate || !dh || !du) return fail(RL_EINVAL, "a required pointer is NULL");
+  if (dgate && !h) return fail(RL_EINVAL, "dgate needs h");
+  const ScanBytes b = scan_bytes(a);
+  const Span in[] = {{gate, b.gate}, {done, b.done}, {h0, b.state}, {h, b.values}, {dh, b.values}, {dh_last, b.state}};
+  const Span out[] = {{du, b.values}, {dgate, b.gate}, {dh0, b.state}, {workspace, workspace_bytes}};
+  if (aliased(in, out, dh_last, dh0)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (!scan_aligned(a, {h, dh, du}, {h0, dh_last, dh0}, gate) || !scan_aligned(a, {}, {}, dgate))
+    return fail(RL_EINVAL, "an array is not aligned to its elements");
+  const size_t need = rl::scan_workspace_bytes(a, true);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
+  return launched(rl::launch_scan_backward(a, gate, done, h0, h, dh, dh_last, du, dgate, dh0, workspace,
+                                           (hipStream_t)stream),
+                  "rl_scan_backward");
+}
+
+size_t rl_ppo_workspace_bytes(const rl_ppo_config* cfg) {
+  if (check_ppo(cfg) != RL_OK) return 0;
+  ok();
+  return rl::ppo_workspace_bytes(cfg->n_rows);
+}
+
+rl_status rl_ppo_loss(const rl_ppo_config* cfg, const float* logits, const uint8_t* legal, const uint8_t* mask,
+                      const int32_t* actions, const float* logp_old, const float* adv, const float* value,
+                      const float* value_old, const float* ret, float* dlogits, float* dvalue, float* stats,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+  const rl_status s = check_ppo(cfg);
+  if (s != RL_OK) return s;
+  if (!logits || !actions || !logp_old || !adv || !value || !ret || !dlogits || !dvalue || !stats)
+    return fail(RL_EINVAL, "a required pointer is NULL");
+  if (cfg->value_clip > 0.f && !value_old) return fail(RL_EINVAL, "value_clip needs value_old");
+  const size_t R = (size_t)cfg->n_rows, na = (size_t)cfg->n_actions;
+  const Span in[] = {{logits, 4 * R * na}, {legal, R * na}, {mask, R}, {actions, 4 * R}, {logp_old, 4 * R},
+                     {adv, 4 * R}, {value, 4 * R}, {value_old, 4 * R}, {ret, 4 * R}};
+  const Span out[] = {{dlogits, 4 * R * na}, {dvalue, 4 * R}, {stats, 24}, {workspace, workspace_bytes}};
+  if (aliased(in, out)) return fail(RL_EINVAL, "an output overlaps another array");
+  const void* words[] = {logits, actions, logp_old, adv, value, value_old, ret, dlogits, dvalue, stats};
+  for (const void* w : words)
+    if (!aligned_to(w, 4)) return fail(RL_EINVAL, "an array is not aligned to its elements");
+  const size_t need = rl::ppo_workspace_bytes(cfg->n_rows);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need)
+    return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
+  const rl::PpoArgs p{cfg->n_rows, cfg->n_actions, cfg->normalize_adv, cfg->clip, cfg->value_clip, cfg->value_coef,
+                      cfg->entropy_coef, logits, legal, mask, actions, logp_old, adv, value,
+                      cfg->value_clip > 0.f ? value_old : nullptr, ret, dlogits, dvalue, stats};
+  return launched(rl::launch_ppo(p, workspace, (hipStream_t)stream), "rl_ppo_loss");
+}
+
+size_t rl_orthogonalize_workspace_bytes(int32_t n, int32_t rows, int32_t cols, int32_t dtype) {
+  const rl::OrthoArgs a{n, rows, cols, dtype, 1};
+  if (check_ortho(a) != RL_OK) return 0;
+  ok();
+  return rl::ortho_workspace_bytes(a);
+}
+
+rl_status rl_orthogonalize(int32_t n, int32_t rows, int32_t cols, int32_t dtype, int32_t steps, const void* g,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const rl::OrthoArgs a{n, rows, cols, dtype, steps};
+  const rl_status s = check_ortho(a);
+  if (s != RL_OK) return s;
+  if (!g || !out) return fail(RL_EINVAL, "a required pointer is NULL");
+  const size_t es = dtype == RL_BF16 ? 2 : 4, bytes = es * (size_t)n * (size_t)rows * (size_t)cols;
+  const Span in[] = {{g, bytes}};
+  const Span outs[] = {{out, bytes}, {workspace, workspace_bytes}};
+  if (aliased(in, outs, g, out)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (!aligned_to(g, es) || !aligned_to(out, es)) return fail(RL_EINVAL, "an array is not aligned to its elements");
+  const size_t need = rl::ortho_workspace_bytes(a);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
+  return launched(rl::launch_ortho(a, g, out, workspace, (hipStream_t)stream), "rl_orthogonalize");
 }
 
 rl_status rollout_run_pop(const rl_env_config* cfg, const rl_policy* pop, int32_t n_policies,

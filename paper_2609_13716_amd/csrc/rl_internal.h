@@ -265,6 +265,48 @@ hipError_t s5_scratch_ptr(void** out);
 hipError_t launch_gae(const float* reward, const uint8_t* done, const float* value, const float* value_last, int T,
                       int E, int A, float gamma, float lambda, float* adv, float* ret, hipStream_t s);
 
+// Linear recurrence over a trajectory and its gradient (rl_scan.hip).
+struct ScanArgs {
+  bool diag;    // one complex factor per channel (else a gate per step and channel)
+  int dt;       // DT_F32 / DT_BF16 of the values
+  int T, E, A;  // steps, envs, agents
+  int W;        // channels of a row (complex ones when diag)
+};
+size_t scan_workspace_bytes(const ScanArgs& p, bool backward);
+hipError_t launch_scan(const ScanArgs& p, const void* u, const void* gate, const uint8_t* done, const float* h0,
+                       void* h, float* h_last, void* workspace, hipStream_t s);
+hipError_t launch_scan_backward(const ScanArgs& p, const void* gate, const uint8_t* done, const float* h0,
+                                const void* h, const void* dh, const float* dh_last, void* du, void* dgate,
+                                float* dh0, void* workspace, hipStream_t s);
+
+// PPO loss and gradients (rl_ppo.hip).
+struct PpoArgs {
+  int64_t R;
+  int NA, normalize;
+  float clip, value_clip, value_coef, entropy_coef;
+  const float* logits;
+  const uint8_t* legal;
+  const uint8_t* mask;
+  const int32_t* actions;
+  const float* logp_old;
+  const float* adv;
+  const float* value;
+  const float* value_old;
+  const float* ret;
+  float* dlogits;
+  float* dvalue;
+  float* stats;
+};
+size_t ppo_workspace_bytes(int64_t R);
+hipError_t launch_ppo(const PpoArgs& p, void* workspace, hipStream_t s);
+
+// Newton-Schulz orthogonalisation (rl_ortho.hip).
+struct OrthoArgs {
+  int n, rows, cols, dt, steps;
+};
+size_t ortho_workspace_bytes(const OrthoArgs& p);
+hipError_t launch_ortho(const OrthoArgs& p, const void* g, void* out, void* workspace, hipStream_t s);
+
 // Population rollout (LBF): agent a of env e acts with policy pidx[e * A + a]
 // of n_pol networks stacked in pol's weight arrays.
 constexpr size_t LBF_POP_STATIC_LDS = 64;  // bytes of static LDS the population kernel may declare

@@ -24,6 +24,7 @@ LIB_PATH = os.environ.get("RL_LIB_PATH") or os.path.join(_HERE, "librollout.so")
 RL_OK, RL_EINVAL, RL_EUNSUPPORTED, RL_ESHAPE, RL_EDEVICE = 0, -1, -2, -3, -4
 RL_ENV_LBF, RL_ENV_OVERCOOKED, RL_ENV_HANABI = 0, 1, 2
 RL_F32, RL_BF16 = 0, 1
+RL_SCAN_GATED, RL_SCAN_DIAGONAL = 0, 1
 
 _TORCH_DT = {RL_F32: torch.float32, RL_BF16: torch.bfloat16}
 _DT_CODE = {"f32": RL_F32, "bf16": RL_BF16, torch.float32: RL_F32, torch.bfloat16: RL_BF16}
@@ -71,6 +72,17 @@ class _S5Policy(ctypes.Structure):
                 ("critic_w", ctypes.c_void_p * 4), ("critic_b", ctypes.c_void_p * 4)]
 
 
+class _ScanConfig(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_steps", ctypes.c_int32),
+                ("n_envs", ctypes.c_int32), ("n_agents", ctypes.c_int32), ("width", ctypes.c_int32)]
+
+
+class _PpoConfig(ctypes.Structure):
+    _fields_ = [("n_rows", ctypes.c_int64), ("n_actions", ctypes.c_int32), ("normalize_adv", ctypes.c_int32),
+                ("clip", ctypes.c_float), ("value_clip", ctypes.c_float), ("value_coef", ctypes.c_float),
+                ("entropy_coef", ctypes.c_float)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -m paper_2609_13716_amd.build`")
@@ -116,6 +128,16 @@ def _load():
     lib.rl_policy_packed_bytes.argtypes = [ctypes.POINTER(_Policy)]
     lib.rl_policy_packed_bytes.restype = ctypes.c_size_t
     lib.rl_policy_pack.argtypes, lib.rl_policy_pack.restype = [ctypes.POINTER(_Policy), P, P], st
+    scp, ppp, i32, sz = ctypes.POINTER(_ScanConfig), ctypes.POINTER(_PpoConfig), ctypes.c_int32, ctypes.c_size_t
+    lib.rl_scan_workspace_bytes.argtypes, lib.rl_scan_workspace_bytes.restype = [scp, i32], sz
+    lib.rl_scan.argtypes, lib.rl_scan.restype = [scp, P, P, P, P, P, P, P, sz, P], st
+    lib.rl_scan_backward.argtypes = [scp, P, P, P, P, P, P, P, P, P, P, sz, P]
+    lib.rl_scan_backward.restype = st
+    lib.rl_ppo_workspace_bytes.argtypes, lib.rl_ppo_workspace_bytes.restype = [ppp], sz
+    lib.rl_ppo_loss.argtypes, lib.rl_ppo_loss.restype = [ppp, P, P, P, P, P, P, P, P, P, P, P, P, P, sz, P], st
+    lib.rl_orthogonalize_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    lib.rl_orthogonalize_workspace_bytes.restype = sz
+    lib.rl_orthogonalize.argtypes, lib.rl_orthogonalize.restype = [i32, i32, i32, i32, i32, P, P, P, sz, P], st
     return lib
 
 
@@ -125,7 +147,9 @@ lib = _load()
 EXPORTED = ("rl_state_bytes", "rl_obs_dim", "rl_num_actions", "rollout_last_error", "rollout_init",
             "rollout_step", "policy_forward", "rollout_run", "rollout_sample", "rl_gumbel_noise", "rollout_run_pop",
             "rollout_run_ac", "rl_gae", "rl_s5_discretize", "rl_s5_workspace_bytes", "rollout_run_s5",
-            "rollout_run_teams", "rl_policy_packed_bytes", "rl_policy_pack", "rollout_run_s5_noalloc")
+            "rollout_run_teams", "rl_policy_packed_bytes", "rl_policy_pack", "rollout_run_s5_noalloc",
+            "rl_scan_workspace_bytes", "rl_scan", "rl_scan_backward", "rl_ppo_workspace_bytes", "rl_ppo_loss",
+            "rl_orthogonalize_workspace_bytes", "rl_orthogonalize")
 HEURISTICS = ("greedy_closest_self", "greedy_closest_teammate", "greedy_closest_avg", "greedy_lowest_level",
               "greedy_highest_level", "seq_lexicographic", "seq_reverse_lexicographic", "seq_column_major",
               "seq_reverse_column_major", "seq_nearest_agent", "seq_farthest_agent")  # kind k of rollout_run_teams
@@ -568,6 +592,199 @@ def gae(reward, done, value, value_last, gamma, lam, adv=None, ret=None, stream=
     _check(lib.rl_gae(_ptr(reward), _ptr(done), _ptr(value), _ptr(value_last), T, E, A, gamma, lam, _ptr(adv),
                       _ptr(ret), _stream(stream)))
     return adv, ret
+
+
+# ---- a learner's operators (see the learner section of include/rollout.h) ----
+
+
+class _On:
+    """Where a learner's call runs: the device its tensors share, and the stream given or that device's current one.
+    Inside the block both are torch's current ones, so what the call allocates belongs to that stream."""
+
+    def __init__(self, stream, **tensors):
+        dev = None
+        for name, t in tensors.items():
+            if t is None:
+                continue
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a device tensor")
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise ValueError(f"{name} is on {t.device}, the tensors before it on {dev}")
+        if stream is not None and stream.device != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on {dev}")
+        self._guards = []
+        if dev.index != torch.cuda.current_device():
+            self._guards.append(torch.cuda.device(dev))
+        if stream is not None:
+            self._guards.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for g in self._guards:
+            g.__enter__()
+
+    def __exit__(self, *exc):
+        for g in reversed(self._guards):
+            g.__exit__(*exc)
+
+
+def _new(t, shape, dtype, like):
+    return torch.empty(shape, dtype=dtype, device=like.device) if t is None else t
+
+
+def _workspace(workspace, nbytes, like):
+    """(tensor or None, its bytes) for a call that needs nbytes; allocated when not given."""
+    if workspace is None:
+        if nbytes == 0:
+            return None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
+    else:
+        _need(workspace, "workspace", torch.uint8)
+    return workspace, workspace.numel()
+
+
+def _scan_config(values, gate, name):
+    """The C config, and the shapes of the states and of the gate, for values [T, E, A, D] (gated) or
+    [T, E, A, 2, P] (diagonal: gate is lambda_bar [2, P])."""
+    if values.dtype not in _DT_CODE:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {values.dtype}")
+    s = tuple(values.shape)
+    diag = gate.dim() == 2
+    if len(s) != (5 if diag else 4) or (diag and s[3] != 2):
+        raise ValueError(f"{name} must be " + ("[T, E, A, 2, P] (the gate is [2, P])" if diag else "[T, E, A, D]") +
+                         f", got {s}")
+    if max(s) > 0x7fffffff:
+        raise ValueError(f"{name} has a size beyond 32 bits: {s}")
+    cfg = _ScanConfig(RL_SCAN_DIAGONAL if diag else RL_SCAN_GATED, _DT_CODE[values.dtype], s[0], s[1], s[2], s[-1])
+    return cfg, (2, s[4]) if diag else s
+
+
+def scan_workspace_bytes(values, gate, backward=False):
+    """Bytes of workspace scan (or scan_backward) needs for values and a gate of these shapes."""
+    cfg, _ = _scan_config(values, gate, "values")
+    return lib.rl_scan_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+def scan(u, gate, done=None, h0=None, h=None, h_last=None, workspace=None, stream=None):
+    """h_t = a_t h_{t-1} + u_t over a trajectory, cut after steps whose done is set; see rl_scan in include/rollout.h.
+
+    u [T, E, A, D] with gate like u, or u [T, E, A, 2, P] with gate = lambda_bar [2, P] float32; done [T, E] uint8;
+    h0 float32, one step's shape.  Returns (h, h_last): the states, and the float32 state the next call starts from
+    (h_last may be h0: the state is advanced in place).  ``workspace``: a uint8 tensor of at least
+    scan_workspace_bytes(u, gate) bytes (allocated when None)."""
+    cfg, gshape = _scan_config(u, gate, "u")
+    T, E, state = u.shape[0], u.shape[1], u.shape[1:]
+    _need(u, "u")
+    _need(gate, "gate", torch.float32 if cfg.kind == RL_SCAN_DIAGONAL else u.dtype, gshape)
+    _need(done, "done", torch.uint8, (T, E))
+    _need(h0, "h0", torch.float32, state)
+    with _On(stream, u=u, gate=gate, done=done, h0=h0, h=h, h_last=h_last, workspace=workspace):
+        h, h_last = _new(h, u.shape, u.dtype, u), _new(h_last, state, torch.float32, u)
+        _need(h, "h", u.dtype, u.shape)
+        _need(h_last, "h_last", torch.float32, state)
+        c = ctypes.byref(cfg)
+        ws, n = _workspace(workspace, lib.rl_scan_workspace_bytes(c, 0), u)
+        _check(lib.rl_scan(c, _ptr(u), _ptr(gate), _ptr(done), _ptr(h0), _ptr(h), _ptr(h_last), _ptr(ws), n,
+                           _stream()))
+    return h, h_last
+
+
+def scan_backward(gate, h, dh, done=None, h0=None, dh_last=None, du=None, dgate=None, dh0=None, workspace=None,
+                  stream=None):
+    """Gradients of scan: from dh (of its h) and dh_last (of its h_last, None: zeros), with gate, done and h0 as given
+    to it and h as it returned it.  Returns (du, dgate, dh0); see rl_scan_backward in include/rollout.h.
+    dh0 may be dh_last.  ``workspace``: at least scan_workspace_bytes(dh, gate, True) bytes (allocated when None)."""
+    cfg, gshape = _scan_config(dh, gate, "dh")
+    T, E, state = dh.shape[0], dh.shape[1], dh.shape[1:]
+    gdt = torch.float32 if cfg.kind == RL_SCAN_DIAGONAL else dh.dtype
+    _need(dh, "dh")
+    _need(h, "h", dh.dtype, dh.shape)
+    _need(gate, "gate", gdt, gshape)
+    _need(done, "done", torch.uint8, (T, E))
+    _need(h0, "h0", torch.float32, state)
+    _need(dh_last, "dh_last", torch.float32, state)
+    with _On(stream, dh=dh, gate=gate, h=h, done=done, h0=h0, dh_last=dh_last, du=du, dgate=dgate, dh0=dh0,
+             workspace=workspace):
+        du, dgate = _new(du, dh.shape, dh.dtype, dh), _new(dgate, gshape, gdt, dh)
+        dh0 = _new(dh0, state, torch.float32, dh)
+        _need(du, "du", dh.dtype, dh.shape)
+        _need(dgate, "dgate", gdt, gshape)
+        _need(dh0, "dh0", torch.float32, state)
+        c = ctypes.byref(cfg)
+        ws, n = _workspace(workspace, lib.rl_scan_workspace_bytes(c, 1), dh)
+        _check(lib.rl_scan_backward(c, _ptr(gate), _ptr(done), _ptr(h0), _ptr(h), _ptr(dh), _ptr(dh_last), _ptr(du),
+                                    _ptr(dgate), _ptr(dh0), _ptr(ws), n, _stream()))
+    return du, dgate, dh0
+
+
+PPO_STATS = ("loss", "policy", "value", "entropy", "approx_kl", "clip_fraction")  # of ppo_loss
+
+
+def ppo_loss(logits, actions, logp_old, adv, value, ret, clip=0.2, value_coef=0.5, entropy_coef=0.01, value_clip=0.0,
+             value_old=None, legal=None, mask=None, normalize=False, dlogits=None, dvalue=None, stats=None,
+             workspace=None, stream=None):
+    """PPO's loss over stored rows and its gradients; see rl_ppo_loss in include/rollout.h.
+
+    logits [.., nA] float32 with any leading shape (a rollout's [T, E, A]); actions int32, logp_old, adv, value, ret
+    and value_old float32 and mask uint8 of that leading shape, legal uint8 like logits.  Returns (dlogits, dvalue,
+    stats), stats [6] named by PPO_STATS.  ``workspace``: uint8, at least ppo_workspace_bytes(logits) bytes
+    (allocated when None)."""
+    lead, na = tuple(logits.shape[:-1]), logits.shape[-1]
+    _need(logits, "logits", torch.float32)
+    _need(actions, "actions", torch.int32, lead)
+    for name, t in (("logp_old", logp_old), ("adv", adv), ("value", value), ("ret", ret), ("value_old", value_old)):
+        _need(t, name, torch.float32, lead)
+    _need(legal, "legal", torch.uint8, logits.shape)
+    _need(mask, "mask", torch.uint8, lead)
+    cfg = _PpoConfig(value.numel(), na, int(normalize), clip, value_clip, value_coef, entropy_coef)
+    with _On(stream, logits=logits, actions=actions, logp_old=logp_old, adv=adv, value=value, ret=ret,
+             value_old=value_old, legal=legal, mask=mask, dlogits=dlogits, dvalue=dvalue, stats=stats,
+             workspace=workspace):
+        dlogits, dvalue = _new(dlogits, logits.shape, torch.float32, logits), _new(dvalue, lead, torch.float32, logits)
+        stats = _new(stats, (6,), torch.float32, logits)
+        _need(dlogits, "dlogits", torch.float32, logits.shape)
+        _need(dvalue, "dvalue", torch.float32, lead)
+        _need(stats, "stats", torch.float32, (6,))
+        c = ctypes.byref(cfg)
+        ws, n = _workspace(workspace, lib.rl_ppo_workspace_bytes(c), logits)
+        _check(lib.rl_ppo_loss(c, _ptr(logits), _ptr(legal), _ptr(mask), _ptr(actions), _ptr(logp_old), _ptr(adv),
+                               _ptr(value), _ptr(value_old), _ptr(ret), _ptr(dlogits), _ptr(dvalue), _ptr(stats),
+                               _ptr(ws), n, _stream()))
+    return dlogits, dvalue, stats
+
+
+def ppo_workspace_bytes(logits):
+    """Bytes of workspace ppo_loss needs for these logits."""
+    cfg = _PpoConfig(logits.numel() // max(logits.shape[-1], 1), logits.shape[-1], 0, 0.2, 0.0, 0.0, 0.0)
+    return lib.rl_ppo_workspace_bytes(ctypes.byref(cfg))
+
+
+def _ortho_sizes(g):
+    if g.dtype not in _DT_CODE:
+        raise ValueError(f"g must be float32 or bfloat16, got {g.dtype}")
+    if g.dim() not in (2, 3):
+        raise ValueError(f"g must be [rows, cols] or [n, rows, cols], got {tuple(g.shape)}")
+    return (g.shape[0] if g.dim() == 3 else 1), g.shape[-2], g.shape[-1], _DT_CODE[g.dtype]
+
+
+def orthogonalize_workspace_bytes(g):
+    """Bytes of workspace orthogonalize needs for g."""
+    return lib.rl_orthogonalize_workspace_bytes(*_ortho_sizes(g))
+
+
+def orthogonalize(g, steps=5, out=None, workspace=None, stream=None):
+    """Newton-Schulz orthogonalisation of a weight update, or of a stack of them ([rows, cols] or [n, rows, cols],
+    float32 or bfloat16); out may be g.  See rl_orthogonalize in include/rollout.h.  ``workspace``: uint8, at least
+    orthogonalize_workspace_bytes(g) bytes (allocated when None)."""
+    sizes = _ortho_sizes(g)
+    _need(g, "g")
+    with _On(stream, g=g, out=out, workspace=workspace):
+        out = _new(out, g.shape, g.dtype, g)
+        _need(out, "out", g.dtype, g.shape)
+        ws, n = _workspace(workspace, lib.rl_orthogonalize_workspace_bytes(*sizes), g)
+        _check(lib.rl_orthogonalize(*sizes, steps, _ptr(g), _ptr(out), _ptr(ws), n, _stream()))
+    return out
 
 
 def rollout_run_pop(cfg, pop, policy_index, state, t0, n_steps, obs=None, actions=None, logits=None, reward=None,

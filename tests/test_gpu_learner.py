@@ -1,0 +1,641 @@
+"""GPU parity of the learner's operators (rl_scan, rl_scan_backward, rl_ppo_loss, rl_orthogonalize) against the float64
+oracle, through the binding.
+
+Tolerances.  u = 2^-24 is float32's half step, 2^-8 bfloat16's; a value rounded to bfloat16 is off by 2^-8 of itself.
+
+Recurrence: a term a_t .. a_{j+1} u_j of h_t goes through at most one product and one sum for each step it passed (for
+a complex factor each real part: two products and two sums, so twice that, over moduli), plus 8 products and sums
+where segments join.  With S_t = sum of the terms' magnitudes and D_t the same weighted by steps passed, the error of
+h_t is at most u (c D_t + 16 S_t), c = 2 real, 4 complex.  The gradient's g is the same recurrence from the end.
+dgate_t = g_t h_{t-1}: |h_{t-1}| times g's bound, and u for the product (4 u complex).  lambda's gradient: the sum of
+those over steps and rows; up to 32 products are added in float32 (32 u of their magnitudes) before float64.
+
+PPO: log p = x - top - log(sum): expf and logf are within 4 steps, so with X the largest magnitude among the row's
+legal logits and old the stored log-probability, log p is within u (16 + 4 X) and log ratio within
+t = u (16 + 4 X + 2 |old|); exp turns that into t + 4 u of the ratio.  A gradient by a logit is
+slope (onehot - p) + c p (log p + H): (t + 16 u) |slope| + c (t + 16 u) (|log p| + H + 2) bounds it.  Means: the mean
+of the rows' bounds.
+
+Orthogonalisation: a rounding u of X_i grows by at most 3.4445 a step (its largest slope on [0, 1.21], at 0), and
+|X_i|_F itself is at most 3.4445^i, so the roundings of all steps end up below (steps + 1) 3.4445^steps u; products
+of k terms are off by up to 16 sqrt(k) u of their size where they do not grow (singular values near 1).  In Frobenius norm:
+(steps + 1) 3.4445^steps u + 16 sqrt(k) u |O|_F, and 2^-8 |O|_F for bfloat16.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import learner as L
+from paper_2609_13716_amd import rollout as R
+
+from parity import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+U32, UBF = 2.0 ** -24, 2.0 ** -8
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    require_gpu()
+
+
+def _offset(t, elements):
+    """t on the GPU, contiguous, starting `elements` elements into its allocation."""
+    buf = torch.empty(t.numel() + elements, dtype=t.dtype, device="cuda")
+    out = buf[elements:].view(t.shape)
+    out.copy_(t)
+    return out
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _cplx(x, axis):
+    x = np.moveaxis(x, axis, -1)
+    return x[..., 0] + 1j * x[..., 1]
+
+
+def _close(got, want, tol, what):
+    err = np.abs(got - want)
+    bad = ~(err <= tol)
+    assert not bad.any(), (what, int(bad.sum()), float(np.nanmax(err - tol)), np.argwhere(bad)[:4].tolist())
+
+
+class Scan:
+    """Inputs of one recurrence on the GPU and their float64 views."""
+
+    def __init__(self, kind, dt, T, E, A, W, done=0.1, h0=True, seed=0, off=0, radius=None):
+        rng = np.random.default_rng(seed)
+        tail = (2, W) if kind == "diagonal" else (W,)
+        self.kind, self.dt = kind, dt
+        mk = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32))  # noqa: E731
+        t = TDT[dt]
+        self.u = _offset(mk(T, E, A, *tail).to(t), off)
+        self.dh = _offset(mk(T, E, A, *tail).to(t), off)
+        if kind == "diagonal":
+            r = rng.uniform(0.8, 1.0, W) if radius is None else np.full(W, radius)
+            ang = rng.uniform(-3, 3, W)
+            gate = torch.from_numpy(np.stack([r * np.cos(ang), r * np.sin(ang)]).astype(np.float32))
+        else:
+            r = 1 / (1 + np.exp(-2 - 1.5 * rng.standard_normal((T, E, A, W)))) if radius is None else \
+                np.full((T, E, A, W), radius)
+            gate = torch.from_numpy((r * np.where(rng.random(r.shape) < 0.1, -1, 1)).astype(np.float32)).to(t)
+        self.gate = _offset(gate, off)
+        self.done = None if done is None else _offset(
+            torch.from_numpy((rng.random((T, E)) < done).astype(np.uint8) * rng.integers(1, 4, (T, E)).astype(np.uint8)),
+            off)
+        self.h0 = _offset(mk(E, A, *tail), off) if h0 else None
+        self.dh_last = _offset(mk(E, A, *tail), off) if h0 else None
+
+    def ref(self, t, state=False):
+        if t is None:
+            return None
+        x = _np(t)
+        return _cplx(x, (2 if state else 3)) if self.kind == "diagonal" else x
+
+    def ref_gate(self):
+        return _cplx(_np(self.gate), 0) if self.kind == "diagonal" else _np(self.gate)
+
+    def ref_done(self):
+        return None if self.done is None else self.done.cpu().numpy()
+
+    @property
+    def c(self):
+        return 4 if self.kind == "diagonal" else 2
+
+    def split(self, x, axis):
+        return np.stack([x.real, x.imag], axis) if self.kind == "diagonal" else x
+
+    def forward_bound(self):
+        return L.path_lengths(self.ref(self.u), self.ref_gate(), self.ref_done(), self.ref(self.h0, True))
+
+    def backward_bound(self):
+        """(S, D) of g: the recurrence from the end, the carried gradient its first state."""
+        dh, gate, done = self.ref(self.dh)[::-1], self.ref_gate(), self.ref_done()
+        T = len(dh)
+        back = np.abs(gate)[None, None, None].repeat(T, 0) * np.ones(dh.shape) if gate.ndim == 1 else np.abs(gate)
+        back = np.concatenate([np.ones_like(back[:1]), back[::-1][:-1]])  # by a_{t+1}; the carried one by 1
+        d2 = None
+        first = self.ref(self.dh_last, True)
+        if done is not None:
+            d2 = np.concatenate([done[::-1][1:], np.zeros_like(done[:1])])  # cut between t+1 and t where done[t]
+            if first is not None:
+                first = np.where((done[-1] != 0)[:, None, None], 0, first)
+        S, D = L.path_lengths(np.abs(dh), back, d2, None if first is None else np.abs(first))
+        return S[::-1], D[::-1]
+
+    def check_forward(self, h, last):
+        want, wlast = L.scan(self.ref(self.u), self.ref_gate(), self.ref_done(), self.ref(self.h0, True))
+        S, D = self.forward_bound()
+        tol = U32 * (self.c * D + 16 * S)
+        if last is not None:
+            _close(_np(last), self.split(wlast, 2), self.split(tol[-1] * (1 + 1j), 2) if self.kind == "diagonal" else tol[-1],
+                   "h_last")
+        if h is not None:
+            half = UBF if self.dt == "bf16" else 0.0
+            w = self.split(want, 3)
+            t = np.stack([tol, tol], 3) if self.kind == "diagonal" else tol
+            _close(_np(h), w, t + half * (np.abs(w) + t), "h")
+
+    def check_backward(self, h, du, dgate, dh0):
+        hr = self.ref(h)
+        wdu, wdg, wd0 = L.scan_backward(self.ref_gate(), hr, self.ref(self.dh), self.ref_done(),
+                                        self.ref(self.h0, True), self.ref(self.dh_last, True))
+        S, D = self.backward_bound()
+        tg = U32 * (self.c * D + 16 * S)
+        half = UBF if self.dt == "bf16" else 0.0
+        wide = lambda x, ax: np.stack([x, x], ax) if self.kind == "diagonal" else x  # noqa: E731
+        w, t = self.split(wdu, 3), wide(tg, 3)
+        _close(_np(du), w, t + half * (np.abs(w) + t), "du")
+        gate = np.abs(self.ref_gate())
+        a0 = gate if gate.ndim == 1 else gate[0]
+        _close(_np(dh0), self.split(wd0, 2), wide(a0 * tg[0] + 4 * U32 * a0 * S[0], 2), "dh0")
+        prev = np.concatenate([np.zeros_like(hr[:1]) if self.h0 is None else self.ref(self.h0, True)[None], hr[:-1]])
+        prev = np.abs(prev)
+        if self.kind == "diagonal":
+            tol = (tg * prev).sum((0, 1, 2)) + 40 * U32 * (S * prev).sum((0, 1, 2))
+            _close(_np(dgate), np.stack([wdg.real, wdg.imag]), np.stack([tol, tol]), "dgate")
+        else:
+            t = tg * prev + U32 * np.abs(wdg)
+            _close(_np(dgate), wdg, t + half * (np.abs(wdg) + t), "dgate")
+
+
+# steps, envs, agents, width: one step; single values; lengths about the loads ahead and the segments; long runs of few
+# channels; odd rows; many channels
+SCAN_SIZES = [(1, 1, 1, 1), (1, 16, 2, 128), (2, 3, 1, 5), (7, 5, 2, 64), (8, 1, 1, 256), (9, 2, 3, 33), (63, 4, 2, 16),
+              (64, 1, 2, 100), (65, 3, 3, 31), (129, 40, 2, 64), (1000, 1, 1, 1), (1023, 2, 1, 64), (4097, 1, 1, 48),
+              (5000, 2, 2, 65), (20000, 1, 1, 8), (128, 300, 2, 128), (3, 700, 3, 77), (513, 16, 1, 256)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+@pytest.mark.parametrize("size", SCAN_SIZES)
+def test_scan_and_gradient(kind, dt, size):
+    seed = sum(size)
+    s = Scan(kind, dt, *size, done=(None, 0.1, 0.02)[seed % 3], h0=seed % 2 == 0, seed=seed, off=(0, 1, 3)[seed // 3 % 3])
+    h, last = R.scan(s.u, s.gate, s.done, s.h0)
+    s.check_forward(h, last)
+    du, dgate, dh0 = R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last)
+    s.check_backward(h, du, dgate, dh0)
+
+
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+@pytest.mark.parametrize("p", [0.0, 0.5, 1.0])
+@pytest.mark.parametrize("size", [(1, 4, 2, 16), (300, 3, 2, 16), (6000, 1, 1, 16), (40, 600, 2, 64)])
+def test_scan_every_episode_border(kind, p, size):
+    """No step, every second step and every step ends an episode; factors of modulus 1 forget nothing by themselves."""
+    s = Scan(kind, "f32", *size, done=p, radius=1.0, seed=int(10 * p))
+    h, last = R.scan(s.u, s.gate, s.done, s.h0)
+    s.check_forward(h, last)
+    s.check_backward(h, *R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last))
+    if p == 1.0:
+        assert torch.equal(h[1:], s.u[1:]) and (last == 0).all()
+
+
+@pytest.mark.parametrize("size", [(70, 4, 2, 64), (6000, 1, 2, 16), (5, 900, 2, 40)])
+def test_scan_cut_states_and_gates_are_not_read(size):
+    """Behind an episode's end neither NaN gates, NaN states nor overflown ones reach the next episode; its gradient
+    by the gate there is 0.  Channels that are not cut keep their NaN."""
+    T, E, A, W = size
+    s = Scan("gated", "f32", *size, done=0.05, seed=3)
+    s.done[T // 2] = 1
+    cut = (s.done[:-1] != 0)[:, :, None, None].expand(T - 1, E, A, W)
+    s.gate[1:][cut] = float("nan")
+    s.u[T // 2, 0, 0, 1] = float("inf")  # the last step of an episode
+    s.u[T // 2, -1, -1, 2] = float("nan")
+    h, last = R.scan(s.u, s.gate, s.done, s.h0)
+    want, wlast = L.scan(_np(s.u), _np(s.gate), s.ref_done(), _np(s.h0))
+    assert np.array_equal(np.isfinite(_np(h)), np.isfinite(want)) and np.isfinite(_np(last)).all()
+    assert int((~np.isfinite(want)).sum()) == 2
+    fine = np.isfinite(want)
+    assert np.allclose(_np(h)[fine], want[fine], rtol=1e-4, atol=1e-4)
+    du, dgate, dh0 = R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last)
+    wdu, wdg, wd0 = L.scan_backward(_np(s.gate), np.where(fine, want, 0.0), _np(s.dh), s.ref_done(), _np(s.h0),
+                                    _np(s.dh_last))
+    assert np.allclose(_np(du), wdu, rtol=1e-4, atol=1e-4) and np.allclose(_np(dh0), wd0, rtol=1e-4, atol=1e-4)
+    assert np.allclose(_np(dgate), wdg, rtol=1e-4, atol=1e-4) and (dgate[1:][cut] == 0).all()
+
+
+def test_scan_nan_stays_in_its_channel():
+    for T, E in ((50, 6), (4000, 1)):
+        s = Scan("gated", "f32", T, E, 2, 32, done=None, seed=4)
+        s.u[T // 3, 0, 1, 5] = float("nan")
+        h, last = R.scan(s.u, s.gate, None, s.h0)
+        bad = torch.isnan(h)
+        assert bad[T // 3:, 0, 1, 5].all() and int(bad.sum()) == T - T // 3 and int(torch.isnan(last).sum()) == 1
+
+
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+def test_scan_optional_arguments(kind):
+    """h or h_last left out, in-place states, dgate or dh0 left out: the other outputs do not change by a bit."""
+    for size in ((1, 8, 2, 64), (33, 5, 2, 24), (5000, 1, 1, 24)):
+        s = Scan(kind, "f32", *size, seed=5)
+        h, last = R.scan(s.u, s.gate, s.done, s.h0)
+        carry = s.h0.clone()
+        h2, l2 = R.scan(s.u, s.gate, s.done, carry, h_last=carry)
+        assert l2 is carry and torch.equal(h2, h) and torch.equal(carry, last)
+        cfg, _ = R._scan_config(s.u, s.gate, "u")
+        c = R.ctypes.byref(cfg)
+        ws = torch.empty(max(R.scan_workspace_bytes(s.u, s.gate), R.scan_workspace_bytes(s.u, s.gate, True), 1),
+                         dtype=torch.uint8, device="cuda")
+        st, p = R._stream(), R._ptr
+        l3, h3 = torch.full_like(last, 7), torch.full_like(h, 7)
+        assert R.lib.rl_scan(c, p(s.u), p(s.gate), p(s.done), p(s.h0), None, p(l3), p(ws), ws.numel(), st) == 0
+        assert R.lib.rl_scan(c, p(s.u), p(s.gate), p(s.done), p(s.h0), p(h3), None, p(ws), ws.numel(), st) == 0
+        assert torch.equal(l3, last) and torch.equal(h3, h)
+        du, dgate, dh0 = R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last)
+        flow = s.dh_last.clone()
+        again = R.scan_backward(s.gate, h, s.dh, s.done, s.h0, flow, dh0=flow)
+        assert again[2] is flow and all(torch.equal(x, y) for x, y in zip(again, (du, dgate, dh0)))
+        du2 = torch.full_like(du, 7)
+        assert R.lib.rl_scan_backward(c, p(s.gate), p(s.done), None, None, p(s.dh), p(s.dh_last), p(du2), None, None,
+                                      p(ws), ws.numel(), st) == 0
+        assert torch.equal(du2, du)
+
+
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+def test_scan_in_pieces(kind):
+    """A trajectory in one call, in two, and step by step with the carried state in place."""
+    s = Scan(kind, "f32", 96, 6, 2, 32, seed=6)
+    carry = s.h0.clone()
+    parts = []
+    for a, b in [(0, 40)] + [(t, t + 1) for t in range(40, 96)]:
+        gate = s.gate if kind == "diagonal" else s.gate[a:b].contiguous()
+        h, _ = R.scan(s.u[a:b], gate, s.done[a:b], carry, h_last=carry)
+        parts.append(h)
+    s.check_forward(torch.cat(parts), carry)
+
+
+def test_scan_gradient_is_the_derivative():
+    """Directional differences of the float32 forward pass in float64 steps: along a random direction of u, gate and h0
+    the loss changes by the inner product with the gradients, to the second order term of the step."""
+    for kind in ("gated", "diagonal"):
+        s = Scan(kind, "f32", 20, 3, 2, 8, seed=7)
+        h, _ = R.scan(s.u, s.gate, s.done, s.h0)
+        du, dgate, dh0 = R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last)
+        rng = np.random.default_rng(8)
+        step = 1e-5
+        vs = [rng.standard_normal(x.shape) for x in (s.u, s.gate, s.h0)]
+        dots = []
+        for sign in (1, -1):
+            u, gate, h0 = (_np(x) + sign * step * v for x, v in zip((s.u, s.gate, s.h0), vs))
+            if kind == "diagonal":
+                hh, ll = L.scan(_cplx(u, 3), _cplx(gate, 0), s.ref_done(), _cplx(h0, 2))
+                hh, ll = np.stack([hh.real, hh.imag], 3), np.stack([ll.real, ll.imag], 2)
+            else:
+                hh, ll = L.scan(u, gate, s.ref_done(), h0)
+            dots.append((hh * _np(s.dh)).sum() + (ll * _np(s.dh_last)).sum())
+        want = (dots[0] - dots[1]) / (2 * step)
+        got = sum((_np(g) * v).sum() for g, v in zip((du, dgate, dh0), vs))
+        assert abs(want - got) < 1e-4 * (1 + abs(want))
+
+
+# ---- PPO ----
+
+
+def _ppo(R_, nA, seed, masked=False, padded=False, spread=2.0, lead=None):
+    rng = np.random.default_rng(seed)
+    x = (spread * rng.standard_normal((R_, nA))).astype(np.float32)
+    legal = None
+    if masked:
+        legal = (rng.random((R_, nA)) < 0.6).astype(np.uint8) * rng.integers(1, 255, (R_, nA)).astype(np.uint8)
+        legal[rng.random(R_) < 0.3] = 0
+        x[(legal == 0) & (rng.random((R_, nA)) < 0.5)] = -np.inf
+        x[(legal == 0) & (rng.random((R_, nA)) < 0.2)] = np.nan
+        x[(legal == 0) & (rng.random((R_, nA)) < 0.2)] = np.finfo(np.float32).min
+    act = rng.integers(0, nA, R_).astype(np.int32)
+    act[rng.random(R_) < 0.02] = -1
+    act[rng.random(R_) < 0.02] = nA + 3
+    f = lambda s=1.0: (s * rng.standard_normal(R_)).astype(np.float32)  # noqa: E731
+    ret = f()
+    vo = ret + f(0.5)
+    kw = dict(logits=x, actions=act, logp_old=(-np.log(nA) + f(0.5)).astype(np.float32), adv=f() + np.float32(0.3),
+              value=vo + f(0.3), ret=ret, value_old=vo, legal=legal,
+              mask=(rng.random(R_) < 0.8).astype(np.uint8) * 3 if padded else None)
+    if padded:  # whatever a padded row holds
+        off = kw["mask"] == 0
+        for k in ("logp_old", "adv", "value", "ret", "value_old"):
+            kw[k][off] = np.nan
+        kw["logits"][off] = np.nan
+    return kw
+
+
+HYPER = dict(clip=0.2, value_coef=0.5, entropy_coef=0.02, value_clip=0.25)
+
+
+def _gpu_args(kw, lead=None, off=0):
+    out = {}
+    for k, v in kw.items():
+        if v is not None:
+            t = torch.from_numpy(v)
+            t = t.reshape(*lead, *t.shape[1:]) if lead else t
+            v = _offset(t, off)
+        out[k] = v
+    return out
+
+
+def _check_ppo(kw, got, normalize, hyper=HYPER):
+    h = {k: float(np.float32(v)) for k, v in hyper.items()}
+    f64 = {k: (v.astype(np.float64) if v is not None and v.dtype == np.float32 else v) for k, v in kw.items()}
+    wdx, wdv, wst = L.ppo_loss(**f64, **h, normalize=normalize)
+    dx, dv, st = (_np(t) for t in got)
+    R_, nA = kw["logits"].shape
+    dx, dv = dx.reshape(R_, nA), dv.reshape(R_)
+    counted = np.ones(R_, bool) if kw["mask"] is None else kw["mask"] != 0
+    n = max(1, counted.sum())
+    x = f64["logits"]
+    ok = ~np.isneginf(x) & counted[:, None]
+    if kw["legal"] is not None:
+        ok &= kw["legal"] != 0
+    X = np.where(ok, np.abs(np.where(ok, x, 0)), 0).max(1)
+    old = np.where(counted, np.abs(np.where(counted, f64["logp_old"], 0)), 0)
+    t = U32 * (16 + 4 * X + 2 * old)
+    adv = np.where(counted, f64["adv"], 0.0)
+    if normalize and counted.any():
+        m = f64["adv"][counted]
+        adv = np.where(counted, (adv - m.mean()) / (m.std() + 1e-8), 0)
+    top = np.where(ok, x, -np.inf).max(1, initial=-np.inf, keepdims=True)
+    with np.errstate(all="ignore"):
+        e = np.where(ok, np.exp(np.where(ok, x - top, 0)), 0)
+        lp = np.where(ok, x - top - np.log(e.sum(1, keepdims=True)), 0)
+    ent = -(np.exp(lp) * lp * ok).sum(1)
+    a = np.clip(kw["actions"], 0, nA - 1)
+    acts = (kw["actions"] == a) & ok[np.arange(R_), a]
+    diff = np.where(acts, lp[np.arange(R_), a] - np.where(counted, f64["logp_old"], 0), 0)
+    ratio = np.where(acts, np.exp(diff), 0)
+    slope = np.abs(adv) * ratio
+    tol = (t + 16 * U32)[:, None] * (slope[:, None] + h["entropy_coef"] * (np.abs(lp) + ent[:, None] + 2)) / n
+    _close(dx, wdx, tol + U32 * np.abs(wdx), "dlogits")
+    _close(dv, wdv, 4 * U32 * np.abs(wdv), "dvalue")
+    assert (dx[~ok] == 0).all() and (dv[~counted] == 0).all()
+    val = wst[2]
+    et = ((t + 16 * U32) * (ent + 2 + np.abs(lp).max(1)) * counted).sum() / n
+    pt = ((t + 16 * U32) * slope).sum() / n
+    kt = ((t + 16 * U32) * (ratio + 1 + np.abs(diff)) * acts).sum() / n
+    tols = np.array([pt + h["value_coef"] * 4 * U32 * val + h["entropy_coef"] * et, pt, 4 * U32 * val, et, kt, 0.0])
+    _close(st, wst, tols + 2 * U32 * np.abs(wst), "stats")
+
+
+@pytest.mark.parametrize("rows,nA", [(1, 6), (2, 1), (3, 32), (64, 2), (255, 6), (256, 20), (257, 7), (1000, 16),
+                                     (5000, 6), (4097, 31), (20011, 20)])
+@pytest.mark.parametrize("masked,padded", [(False, False), (True, False), (False, True), (True, True)])
+def test_ppo(rows, nA, masked, padded):
+    for normalize in (False, True):
+        kw = _ppo(rows, nA, seed=rows + nA, masked=masked, padded=padded)
+        got = R.ppo_loss(**_gpu_args(kw, off=rows % 4), **HYPER, normalize=normalize)
+        _check_ppo(kw, got, normalize)
+
+
+def test_ppo_trajectory_shapes_and_large_batch():
+    T, E, A = 64, 900, 2
+    kw = _ppo(T * E * A, 6, seed=1)
+    got = R.ppo_loss(**_gpu_args(kw, lead=(T, E, A)), **HYPER, normalize=True)
+    assert got[0].shape == (T, E, A, 6) and got[1].shape == (T, E, A)
+    _check_ppo(kw, got, True)
+
+
+def test_ppo_extremes():
+    """Large logits, certain policies, no value clip, no counted row, no legal action anywhere, one legal action."""
+    kw = _ppo(700, 9, seed=2, spread=60.0)
+    kw["logp_old"] = np.maximum(kw["logp_old"], -5).astype(np.float32)
+    hyper = dict(HYPER, value_clip=0.0)
+    args = _gpu_args(kw)
+    args.pop("value_old")
+    _check_ppo(kw, R.ppo_loss(**args, **hyper), False, hyper)
+    kw = _ppo(300, 6, seed=3, masked=True)
+    kw["legal"][:] = 0
+    _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True), True)
+    kw["legal"][:, 2] = 1
+    kw["logits"][:, 2] = 3.0
+    kw["actions"][:] = 2
+    _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True), True)
+    kw = _ppo(300, 6, seed=4, padded=True)
+    kw["mask"][:] = 0
+    got = R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True)
+    assert all((t == 0).all() for t in got)
+    kw = _ppo(300, 6, seed=5)
+    kw["logits"][:] = -np.inf
+    _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER), False)
+
+
+def test_ppo_borders():
+    """Ratios that lie within a few float32 steps of 1 -+ clip: the side is float64's, for every row."""
+    R_, nA = 4000, 6
+    kw = _ppo(R_, nA, seed=6)
+    x = kw["logits"].astype(np.float64)
+    act = np.clip(kw["actions"], 0, nA - 1)
+    kw["actions"] = act.astype(np.int32)
+    lp = x - np.log(np.exp(x).sum(1, keepdims=True))
+    border = np.where(np.arange(R_) % 2 == 0, 0.8, 1.2)
+    old = (lp[np.arange(R_), act] - np.log(border)).astype(np.float32)
+    for k in (-2, -1, 0, 1, 2):  # so many steps of the stored value to either side
+        kw["logp_old"] = (old + k * np.spacing(old)).astype(np.float32)
+        _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER), False)
+    vo, vc = kw["value_old"], np.float32(HYPER["value_clip"])
+    for k in (-1, 0, 1):
+        edge = (vo + np.where(np.arange(R_) % 2 == 0, vc, -vc)).astype(np.float32)
+        kw["value"] = (edge + k * np.spacing(edge)).astype(np.float32)
+        _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER), False)
+
+
+def test_ppo_nan_stays_in_its_row():
+    kw = _ppo(500, 6, seed=7)
+    clean = R.ppo_loss(**_gpu_args(kw), **HYPER)
+    kw["logits"][17, 3] = np.nan
+    dx, dv, st = R.ppo_loss(**_gpu_args(kw), **HYPER)
+    rest = torch.arange(500, device="cuda") != 17
+    assert torch.isnan(dx[17]).all() and torch.equal(dx[rest], clean[0][rest]) and torch.equal(dv, clean[1])
+    assert torch.isnan(st[0]) and torch.isnan(st[3]) and torch.equal(st[2], clean[2][2])
+
+
+# ---- orthogonalisation ----
+
+
+def _matrix(kind, n, r, c, rng):
+    g = rng.standard_normal((n, r, c))
+    k = min(r, c)
+    if kind == "lowrank":
+        q = max(1, k // 8)
+        g = rng.standard_normal((n, r, q)) @ rng.standard_normal((n, q, c)) + 1e-3 * g
+    if kind == "decay":
+        u, _, v = np.linalg.svd(g, full_matrices=False)
+        g = (u * np.logspace(0, -5, k)) @ v
+    return g
+
+
+def _check_ortho(g, out, steps=5):
+    want = L.orthogonalize(_np(g), steps)
+    got = _np(out)
+    if want.ndim == 2:
+        want, got = want[None], got[None]
+    k = max(g.shape[-2:])
+    for i in range(len(want)):
+        size = np.sqrt((want[i] ** 2).sum())
+        tol = (steps + 1) * 3.4445 ** steps * U32 + 16 * np.sqrt(k) * U32 * size
+        if g.dtype == torch.bfloat16:
+            tol += UBF * size
+        err = np.sqrt(((got[i] - want[i]) ** 2).sum())
+        assert err <= tol, (i, tuple(g.shape), err, tol)
+
+
+ORTHO_SIZES = [(1, 1, 1), (1, 1, 300), (2, 6, 128), (3, 128, 6), (1, 7, 7), (2, 16, 16), (1, 31, 33), (5, 64, 192),
+               (9, 128, 192), (2, 192, 128), (1, 128, 128), (2, 129, 130), (1, 127, 1000), (1, 257, 96), (1, 200, 658),
+               (1, 512, 278), (2, 300, 300), (1, 512, 1024), (40, 20, 48), (1, 17, 2049)]
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", ORTHO_SIZES)
+def test_orthogonalize(size, dt):
+    rng = np.random.default_rng(sum(size))
+    for kind, scale in (("normal", 1.0), ("lowrank", 1e-6), ("decay", 1e4)):
+        g = _offset(torch.from_numpy((scale * _matrix(kind, *size, rng)).astype(np.float32)).to(TDT[dt]), sum(size) % 3)
+        _check_ortho(g, R.orthogonalize(g))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+def test_orthogonalize_steps(steps):
+    rng = np.random.default_rng(steps)
+    for size in ((2, 48, 80), (1, 150, 140)):
+        g = torch.from_numpy(rng.standard_normal(size).astype(np.float32)).cuda()
+        _check_ortho(g, R.orthogonalize(g, steps), steps)
+
+
+@pytest.mark.parametrize("size", [(3, 40, 56), (3, 150, 200)])
+def test_orthogonalize_special_matrices(size):
+    """A zero matrix gives zeros, one with a NaN or infinity gives NaN, and the others of the stack keep their bits;
+    scaling by a power of two changes nothing; out may be g; two dimensions or a stack of one are the same."""
+    rng = np.random.default_rng(9)
+    g = torch.from_numpy(rng.standard_normal(size).astype(np.float32)).cuda()
+    clean = R.orthogonalize(g)
+    assert torch.equal(R.orthogonalize(g * 2.0 ** 40), clean) and torch.equal(R.orthogonalize(g * 2.0 ** -60), clean)
+    assert torch.equal(R.orthogonalize(g[1].clone()), clean[1])
+    for bad in (float("nan"), float("inf")):
+        h = g.clone()
+        h[1, 3, 4] = bad
+        h[2] = 0
+        out = R.orthogonalize(h)
+        assert torch.isnan(out[1]).all() and (out[2] == 0).all() and torch.equal(out[0], clean[0])
+    h = g.clone()
+    assert R.orthogonalize(h, out=h) is h and torch.equal(h, clean)
+    big = g / g.abs().max() * 1e38  # |G|_F overflows float32
+    _check_ortho(big, R.orthogonalize(big))
+
+
+# ---- streams, graphs, repeated calls ----
+
+
+def _calls():
+    """(name, call(outputs), outputs): one call of every operator into fixed buffers with its own workspace."""
+    out = []
+    for kind, size in (("gated", (40, 30, 2, 64)), ("diagonal", (40, 30, 2, 64)), ("gated", (6000, 1, 1, 32)),
+                       ("diagonal", (6000, 1, 1, 32))):
+        s = Scan(kind, "f32", *size, seed=10)
+        h, last = torch.empty_like(s.u), torch.empty_like(s.h0)
+        du, dg, d0 = torch.empty_like(s.u), torch.empty_like(s.gate), torch.empty_like(s.h0)
+        ws = torch.empty(max(R.scan_workspace_bytes(s.u, s.gate), 16), dtype=torch.uint8, device="cuda")
+        wb = torch.empty(max(R.scan_workspace_bytes(s.u, s.gate, True), 16), dtype=torch.uint8, device="cuda")
+
+        def call(s=s, h=h, last=last, du=du, dg=dg, d0=d0, ws=ws, wb=wb):
+            R.scan(s.u, s.gate, s.done, s.h0, h=h, h_last=last, workspace=ws)
+            R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last, du=du, dgate=dg, dh0=d0, workspace=wb)
+        out.append((f"scan {kind} {size}", call, [h, last, du, dg, d0]))
+    for rows in (300, 50000):
+        a = _gpu_args(_ppo(rows, 6, seed=11, masked=True, padded=True))
+        dx, dv, st = torch.empty_like(a["logits"]), torch.empty_like(a["value"]), torch.empty(6, device="cuda")
+        wp = torch.empty(R.ppo_workspace_bytes(a["logits"]), dtype=torch.uint8, device="cuda")
+
+        def call(a=a, dx=dx, dv=dv, st=st, wp=wp):
+            R.ppo_loss(**a, **HYPER, normalize=True, dlogits=dx, dvalue=dv, stats=st, workspace=wp)
+        out.append((f"ppo {rows}", call, [dx, dv, st]))
+    for size in ((4, 64, 96), (2, 260, 300)):
+        g = torch.randn(size, device="cuda")
+        o = torch.empty_like(g)
+        wo = torch.empty(max(R.orthogonalize_workspace_bytes(g), 16), dtype=torch.uint8, device="cuda")
+
+        def call(g=g, o=o, wo=wo):
+            R.orthogonalize(g, out=o, workspace=wo)
+        out.append((f"ortho {size}", call, [o]))
+    return out
+
+
+def _same(a, b):
+    return all(torch.equal(x.view(torch.int32), y.view(torch.int32)) for x, y in zip(a, b))
+
+
+def test_equal_calls_give_equal_bits():
+    for name, call, outs in _calls():
+        call()
+        first = [t.clone() for t in outs]
+        for _ in range(3):
+            for t in outs:
+                t.fill_(3.0)
+            call()
+            assert _same(outs, first), name
+
+
+def test_captured_and_replayed():
+    """Each operator in a graph of its own, replayed with eager work of its own between the replays."""
+    for name, call, outs in _calls():
+        call()
+        torch.cuda.synchronize()
+        first = [t.clone() for t in outs]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        for k in range(4):
+            for t in outs:
+                t.fill_(float(k))
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert _same(outs, first), (name, k)
+            call()
+            assert _same(outs, first), (name, k)
+
+
+def test_two_streams_at_once():
+    """Calls on two streams with workspaces of their own, and one whose workspace and outputs the binding allocates."""
+    s = Scan("gated", "f32", 6000, 1, 1, 32, seed=12)
+    p = Scan("diagonal", "f32", 64, 200, 2, 64, seed=13)
+    g = torch.randn(2, 260, 300, device="cuda")
+    want = (R.scan(s.u, s.gate, s.done, s.h0), R.scan_backward(p.gate, p.u, p.dh, p.done, p.h0, p.dh_last),
+            R.orthogonalize(g))
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        got = []
+        for stream in (a, b):
+            got.append((R.scan(s.u, s.gate, s.done, s.h0, stream=stream),
+                        R.scan_backward(p.gate, p.u, p.dh, p.done, p.h0, p.dh_last, stream=stream),
+                        R.orthogonalize(g, stream=stream)))
+        torch.cuda.synchronize()
+        for x in got:
+            assert _same(x[0], want[0]) and _same(x[1], want[1]) and torch.equal(x[2], want[2])
+
+
+def test_binding_checks_on_the_gpu():
+    z = lambda *s, dt=torch.float32: torch.zeros(*s, dtype=dt, device="cuda")  # noqa: E731
+    u = z(4, 2, 2, 8)
+    for bad in (lambda: R.scan(u.transpose(0, 1), z(2, 4, 2, 8)), lambda: R.scan(u, z(4, 2, 2, 7)),
+                lambda: R.scan(u, u.to(torch.bfloat16)), lambda: R.scan(u, z(4, 2, 2, 8), z(4, 2)),
+                lambda: R.scan(u, z(4, 2, 2, 8), z(4, 3, dt=torch.uint8)),
+                lambda: R.scan(u, z(4, 2, 2, 8), h0=z(2, 2, 8, dt=torch.bfloat16)),
+                lambda: R.scan(u, z(4, 2, 2, 8), h=z(4, 2, 2, 9)), lambda: R.scan(u, z(4, 2, 2, 8).cpu()),
+                lambda: R.scan(u, z(4, 2, 2, 8), workspace=z(16)),
+                lambda: R.scan_backward(u, z(4, 2, 2, 8), z(4, 2, 2, 8), dh0=z(2, 2, 9)),
+                lambda: R.ppo_loss(z(5, 6), z(5), z(5), z(5), z(5), z(5)),
+                lambda: R.ppo_loss(z(5, 6), z(4, dt=torch.int32), z(5), z(5), z(5), z(5)),
+                lambda: R.ppo_loss(z(5, 6), z(5, dt=torch.int32), z(5), z(5), z(5), z(5), stats=z(5)),
+                lambda: R.orthogonalize(z(4, 6).t()), lambda: R.orthogonalize(z(4, 6), out=z(6, 4))):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: R.scan(u, z(4, 2, 2, 8), h=u), lambda: R.ppo_loss(z(5, 33), z(5, dt=torch.int32), *[z(5)] * 4),
+                lambda: R.orthogonalize(z(4, 6), steps=0),
+                lambda: R.orthogonalize(z(300, 600), workspace=z(16, dt=torch.uint8)),
+                lambda: R.ppo_loss(z(5, 6), z(5, dt=torch.int32), z(5), z(5), z(5), z(5), clip=float("nan"))):
+        with pytest.raises(R.RolloutError):
+            bad()
