@@ -272,8 +272,8 @@ rl_status rl_gae(const float* reward, const uint8_t* done, const float* value, c
  * rounding, not to the bit; gates are expected not to let the product of
  * a segment's gates overflow float32 (|a| <= 1 never does).  Equal calls give equal
  * bits.
- * Limits: sizes >= 1; n_envs * n_agents * width (twice that for
- * RL_SCAN_DIAGONAL) < 2^31. */
+ * Limits: sizes >= 1; n_steps <= 2^30; n_envs * n_agents * width (twice that
+ * for RL_SCAN_DIAGONAL) < 2^31. */
 enum { RL_SCAN_GATED = 0, RL_SCAN_DIAGONAL = 1 };
 typedef struct {
   int32_t kind;     /* RL_SCAN_* */

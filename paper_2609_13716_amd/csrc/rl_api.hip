@@ -225,6 +225,7 @@ rl_status check_scan(const rl_scan_config* cfg, rl::ScanArgs* a) {
   if (!valid_dtype(cfg->dtype)) return fail(RL_EUNSUPPORTED, "scan dtype %d is not known", cfg->dtype);
   if (cfg->n_steps < 1 || cfg->n_envs < 1 || cfg->n_agents < 1 || cfg->width < 1)
     return fail(RL_EINVAL, "sizes must be >= 1");
+  if (cfg->n_steps > 1 << 30) return fail(RL_EINVAL, "n_steps %d exceeds 2^30", cfg->n_steps);
   const bool diag = cfg->kind == RL_SCAN_DIAGONAL;
   const int64_t most = INT32_MAX;  // divided step by step: the product itself may pass 64 bits
   if (cfg->n_agents > most / cfg->n_envs || cfg->width > most / ((int64_t)cfg->n_envs * cfg->n_agents * (diag ? 2 : 1)))

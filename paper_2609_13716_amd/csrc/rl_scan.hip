@@ -1,13 +1,34 @@
 // Linear recurrence h_t = a_t k_t h_{t-1} + u_t over a trajectory, and its
-// gradient: one thread per channel (a pair of values when the factors are
-// complex), walking over the steps.
+// gradient.
+//
+// A step is an affine map of the carried state (h -> a h + u; backwards, with
+// f the gradient that arrives from later steps, f -> a (dh + f)), and maps
+// compose: (A1, B1) then (A2, B2) is (A2 A1, A2 B1 + B2).  Both passes touch
+// each value once per direction, 2 to 4 floating operations against 4 to 12
+// bytes, so HBM bounds them and what matters is bytes in flight:
+//   * lanes of a wave hold neighbouring channels (one dword per lane and step:
+//     a float, or two bfloat16 of one row), so each access is 256 contiguous
+//     bytes;
+//   * a wave walks SCAN_K steps at a time whose inputs were loaded while the
+//     SCAN_K steps before them were computed;
+//   * with few channels the steps are split: S waves of a workgroup take
+//     SCAN_K consecutive steps each, fold them to one map, exchange the maps
+//     through LDS and replay their steps from the state that reaches them
+//     (inputs stay in registers, so they are read once); and with very few
+//     channels the trajectory is cut into segments, one workgroup each, whose
+//     maps a first launch writes to the workspace (inputs are read twice).
+// Episode ends cut the state: a map that contains one does not read its input.
+// It is marked by SCAN_CUT in place of A, so that 0 * NaN never arises.
+#include <initializer_list>
+
 #include "rl_internal.h"
 
 namespace rl {
 namespace {
 
-constexpr int SCAN_NT = 64;  // one wave per workgroup: channels spread over as many CUs as possible
-constexpr int SCAN_U = 8;    // steps whose inputs are loaded ahead of the dependent recurrence
+constexpr int SCAN_K = 8;           // steps a wave holds in registers
+constexpr int SCAN_S = 16;          // waves of a workgroup that split the steps
+constexpr uint32_t SCAN_CUT = 0x7fc0dead;  // a NaN that stands for "the state before is cut off"
 
 // A channel's value: one float, or a complex number.
 template <bool DIAG>
@@ -16,152 +37,503 @@ template <>
 struct Val<false> {
   float x;
   __device__ static Val zero() { return {0.f}; }
+  __device__ static Val one() { return {1.f}; }
   __device__ static Val add(Val a, Val b) { return {a.x + b.x}; }
-  // a * h + u
+  __device__ static Val mul(Val a, Val b) { return {a.x * b.x}; }
   __device__ static Val fma(Val a, Val h, Val u) { return {fmaf(a.x, h.x, u.x)}; }
-  // conj(a) * h + u
-  __device__ static Val fmac(Val a, Val h, Val u) { return {fmaf(a.x, h.x, u.x)}; }
+  __device__ Val conj() const { return *this; }
 };
 template <>
 struct Val<true> {
   float x, y;
   __device__ static Val zero() { return {0.f, 0.f}; }
+  __device__ static Val one() { return {1.f, 0.f}; }
   __device__ static Val add(Val a, Val b) { return {a.x + b.x, a.y + b.y}; }
+  __device__ static Val mul(Val a, Val b) { return {fmaf(a.x, b.x, -a.y * b.y), fmaf(a.x, b.y, a.y * b.x)}; }
   __device__ static Val fma(Val a, Val h, Val u) {
     return {fmaf(a.x, h.x, fmaf(-a.y, h.y, u.x)), fmaf(a.x, h.y, fmaf(a.y, h.x, u.y))};
   }
-  __device__ static Val fmac(Val a, Val h, Val u) {
-    return {fmaf(a.x, h.x, fmaf(a.y, h.y, u.x)), fmaf(a.x, h.y, fmaf(-a.y, h.x, u.y))};
+  __device__ Val conj() const { return {x, -y}; }
+};
+
+// An affine map of the carried state, or (a cut one) a constant.
+template <bool DIAG>
+struct Map {
+  using V = Val<DIAG>;
+  V a, b;
+  __device__ static Map constant(V b) {
+    V a = V::zero();
+    a.x = __uint_as_float(SCAN_CUT);
+    return {a, b};
+  }
+  __device__ bool cut() const { return __float_as_uint(a.x) == SCAN_CUT; }
+  __device__ V operator()(V h) const { return cut() ? b : V::fma(a, h, b); }
+  // this map after m
+  __device__ Map after(const Map& m) const {
+    if (cut()) return *this;
+    if (m.cut()) return constant(V::fma(a, m.b, b));
+    return {V::mul(a, m.a), V::fma(a, m.b, b)};
   }
 };
 
-template <int DT, bool DIAG>
-__device__ __forceinline__ Val<DIAG> load_val(const void* base, size_t i, int W) {
-  using E = typename DType<DT>::T;
-  const E* p = static_cast<const E*>(base) + i;
-  if constexpr (DIAG) return {DType<DT>::to_f32(p[0]), DType<DT>::to_f32(p[W])};
-  else return {DType<DT>::to_f32(p[0])};
-}
-template <int DT, bool DIAG>
-__device__ __forceinline__ void store_val(void* base, size_t i, int W, Val<DIAG> v) {
-  using E = typename DType<DT>::T;
-  E* p = static_cast<E*>(base) + i;
-  p[0] = DType<DT>::from_f32(v.x);
-  if constexpr (DIAG) p[W] = DType<DT>::from_f32(v.y);
+// The map folded from steps with product a and end value b, of which one was
+// cut (or not): a product that happens to be the marker becomes another NaN.
+template <bool DIAG>
+__device__ __forceinline__ Map<DIAG> folded(Val<DIAG> a, Val<DIAG> b, bool cut) {
+  Map<DIAG> m{a, b};
+  if (cut) return Map<DIAG>::constant(b);
+  if (m.cut()) m.a.x = __uint_as_float(0x7fc00000u);
+  return m;
 }
 
-// Where channel c of a step lies: its offset in the step's values, its env.
-template <bool DIAG>
-struct Chan {
-  int off, p, env;
-  __device__ Chan(const ScanArgs& a, int c) {
+// The V neighbouring channels of a lane (of one row) at a step, as loaded:
+// one dword, or two for complex values (real and imaginary parts).
+template <int DT, bool DIAG, int V>
+struct Raw {
+  uint32_t w[DIAG ? 2 : 1];
+  __device__ Val<DIAG> get(int v) const {
+    auto f = [&](uint32_t x) {
+      if constexpr (DT == DT_F32) return __uint_as_float(x);
+      else return __uint_as_float(v == 0 ? x << 16 : x & 0xffff0000u);
+    };
+    if constexpr (DIAG) return {f(w[0]), f(w[1])};
+    else return {f(w[0])};
+  }
+};
+
+template <int DT>
+constexpr int elem_bytes() { return DT == DT_F32 ? 4 : 2; }
+
+// Where a lane's channels lie.  Steps are M elements apart; off0 is the
+// element offset (in a step) of the workgroup's first lane, uniform, so that
+// addresses are a scalar base plus a 32-bit lane offset.
+template <bool DIAG, int V>
+struct Lane {
+  int c, p;          // first channel, its place in the row
+  int env;
+  size_t off0, M;
+  uint32_t rel;      // elements from off0
+  bool live;         // lanes past the last channel repeat the last one and store nothing
+  __device__ Lane(const ScanArgs& a, int lane) {
+    const int N = a.E * a.A * a.W;
+    const int64_t ci = ((int64_t)blockIdx.x * 64 + lane) * V;
+    live = ci < N;
+    c = live ? (int)ci : N - V;
     const int row = c / a.W;
     p = c - row * a.W;
-    off = DIAG ? row * 2 * a.W + p : c;
     env = row / a.A;
+    M = (size_t)N * (DIAG ? 2 : 1);
+    const int64_t c0 = (int64_t)blockIdx.x * 64 * V;  // the first lane's channel: always < N
+    const int row0 = (int)(c0 / a.W);
+    off0 = (size_t)c0 + (DIAG ? (size_t)row0 * a.W : 0);
+    rel = (uint32_t)((size_t)c + (DIAG ? (size_t)row * a.W : 0) - off0);
   }
 };
 
-template <int DT, bool DIAG>
-__global__ __launch_bounds__(SCAN_NT) void scan_kernel(ScanArgs a, const void* u, const void* gate,
-                                                       const uint8_t* done, const float* h0, void* h,
-                                                       float* h_last) {
-  const int N = a.E * a.A * a.W;
-  const int64_t ci = (int64_t)blockIdx.x * SCAN_NT + threadIdx.x;
-  if (ci >= N) return;
-  const Chan<DIAG> ch(a, (int)ci);
-  const size_t M = (size_t)N * (DIAG ? 2 : 1);
-  using V = Val<DIAG>;
-  V st = h0 ? load_val<DT_F32, DIAG>(h0, ch.off, a.W) : V::zero();
-  V g = V::zero();
-  if constexpr (DIAG) g = load_val<DT_F32, true>(gate, ch.p, a.W);
-  bool keep = true;
-  for (int t0 = 0; t0 < a.T; t0 += SCAN_U) {
-    V in[SCAN_U], ga[SCAN_U];
-    bool go[SCAN_U];
+template <int DT, bool DIAG, int V>
+__device__ __forceinline__ Raw<DT, DIAG, V> load_raw(const void* base, const Lane<DIAG, V>& l, int t, int W) {
+  constexpr int ES = elem_bytes<DT>();
+  const char* s = static_cast<const char*>(base) + ((size_t)t * l.M + l.off0) * ES;
+  Raw<DT, DIAG, V> r;
 #pragma unroll
-    for (int k = 0; k < SCAN_U; ++k) {
-      const int t = t0 + k;
-      if (t < a.T) {
-        in[k] = load_val<DT, DIAG>(u, (size_t)t * M + ch.off, a.W);
-        if constexpr (DIAG) ga[k] = g;
-        else ga[k] = load_val<DT, false>(gate, (size_t)t * M + ch.off, a.W);
-        go[k] = !done || done[(size_t)t * a.E + ch.env] == 0;
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < SCAN_U; ++k) {
-      const int t = t0 + k;
-      if (t < a.T) {
-        st = keep ? V::fma(ga[k], st, in[k]) : in[k];
-        keep = go[k];
-        if (h) store_val<DT, DIAG>(h, (size_t)t * M + ch.off, a.W, st);
-      }
-    }
+  for (int i = 0; i < (DIAG ? 2 : 1); ++i) {
+    const char* q = s + (size_t)i * W * ES + l.rel * (uint32_t)ES;
+    if constexpr (ES * V == 4) r.w[i] = *reinterpret_cast<const uint32_t*>(q);
+    else r.w[i] = *reinterpret_cast<const uint16_t*>(q);
   }
-  if (h_last) store_val<DT_F32, DIAG>(h_last, ch.off, a.W, keep ? st : V::zero());
+  return r;
 }
 
-// dlam_part (diagonal kind): the channel's sum of g conj(k h) over the steps.
-template <int DT, bool DIAG>
-__global__ __launch_bounds__(SCAN_NT) void scan_bwd_kernel(ScanArgs a, const void* gate, const uint8_t* done,
-                                                           const float* h0, const void* h, const void* dh,
-                                                           const float* dh_last, void* du, void* dgate, float* dh0,
-                                                           double* dlam_part) {
-  const int N = a.E * a.A * a.W;
-  const int64_t ci = (int64_t)blockIdx.x * SCAN_NT + threadIdx.x;
-  if (ci >= N) return;
-  const Chan<DIAG> ch(a, (int)ci);
-  const size_t M = (size_t)N * (DIAG ? 2 : 1);
-  using V = Val<DIAG>;
-  V lam = V::zero();
-  if constexpr (DIAG) lam = load_val<DT_F32, true>(gate, ch.p, a.W);
-  double sx = 0., sy = 0.;
-  // gradient that reaches h_t from the steps after it
-  V flow = dh_last && !(done && done[(size_t)(a.T - 1) * a.E + ch.env]) ? load_val<DT_F32, DIAG>(dh_last, ch.off, a.W)
-                                                                          : V::zero();
-  for (int t1 = a.T; t1 > 0; t1 -= SCAN_U) {
-    V in[SCAN_U], ga[SCAN_U], prev[SCAN_U];
-    bool go[SCAN_U];
+template <int DT, bool DIAG, int V>
+__device__ __forceinline__ void store_vals(void* base, const Lane<DIAG, V>& l, int t, int W, const Val<DIAG> (&v)[V]) {
+  constexpr int ES = elem_bytes<DT>();
+  char* s = static_cast<char*>(base) + ((size_t)t * l.M + l.off0) * ES;
+  auto put = [&](char* q, float a, float b) {
+    if constexpr (DT == DT_F32) *reinterpret_cast<float*>(q) = a;
+    else if constexpr (V == 2) *reinterpret_cast<uint32_t*>(q) = pack_bf16x2(a, b);
+    else *reinterpret_cast<uint16_t*>(q) = f32_to_bf16(a);
+  };
+  put(s + l.rel * (uint32_t)ES, v[0].x, v[V - 1].x);
+  if constexpr (DIAG) put(s + (size_t)W * ES + l.rel * (uint32_t)ES, v[0].y, v[V - 1].y);
+}
+
+// A lane's float32 states.
+template <bool DIAG, int V>
+__device__ __forceinline__ void load_state(const float* base, const Lane<DIAG, V>& l, int W, Val<DIAG> (&v)[V]) {
 #pragma unroll
-    for (int k = 0; k < SCAN_U; ++k) {
-      const int t = t1 - 1 - k;
-      if (t >= 0) {
-        in[k] = load_val<DT, DIAG>(dh, (size_t)t * M + ch.off, a.W);
-        if constexpr (DIAG) ga[k] = lam;
-        else ga[k] = load_val<DT, false>(gate, (size_t)t * M + ch.off, a.W);
-        go[k] = t == 0 || !done || done[(size_t)(t - 1) * a.E + ch.env] == 0;
-        prev[k] = V::zero();
-        if (dgate) {
-          if (t > 0) prev[k] = load_val<DT, DIAG>(h, (size_t)(t - 1) * M + ch.off, a.W);
-          else if (h0) prev[k] = load_val<DT_F32, DIAG>(h0, ch.off, a.W);
-        }
-      }
+  for (int i = 0; i < V; ++i) {
+    v[i] = Val<DIAG>::zero();
+    if (base) {
+      v[i].x = base[l.off0 + l.rel + i];
+      if constexpr (DIAG) v[i].y = base[l.off0 + l.rel + i + W];
     }
+  }
+}
+template <bool DIAG, int V>
+__device__ __forceinline__ void store_state(float* base, const Lane<DIAG, V>& l, int W, const Val<DIAG> (&v)[V]) {
 #pragma unroll
-    for (int k = 0; k < SCAN_U; ++k) {
-      const int t = t1 - 1 - k;
-      if (t >= 0) {
-        const V g = V::add(in[k], flow);
-        const bool has = go[k] && (t > 0 || h0);
-        store_val<DT, DIAG>(du, (size_t)t * M + ch.off, a.W, g);
-        if constexpr (DIAG) {
-          if (has) {
-            sx += (double)fmaf(g.x, prev[k].x, g.y * prev[k].y);
-            sy += (double)fmaf(g.y, prev[k].x, -g.x * prev[k].y);
-          }
-        } else if (dgate) {
-          store_val<DT, false>(dgate, (size_t)t * M + ch.off, a.W, has ? V{g.x * prev[k].x} : V::zero());
-        }
-        flow = go[k] ? V::fmac(ga[k], g, V::zero()) : V::zero();
+  for (int i = 0; i < V; ++i) {
+    base[l.off0 + l.rel + i] = v[i].x;
+    if constexpr (DIAG) base[l.off0 + l.rel + i + W] = v[i].y;
+  }
+}
+
+// The maps of a workgroup's waves, exchanged through LDS.  `into` is the state
+// that reaches wave w when `carry` enters the first one, and carry becomes the
+// state that leaves the last one.  Two buffers, so one barrier per exchange:
+// a wave that writes buffer b again has passed the barrier of the exchange in
+// between, which every wave reaches after reading b.
+template <bool DIAG, int V, int S>
+struct Exchange {
+  Map<DIAG> m[2][S][V][64];
+  __device__ void share(int buf, int w, int lane, const Map<DIAG> (&mine)[V]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) m[buf][w][v][lane] = mine[v];
+    __syncthreads();
+  }
+  __device__ void operator()(int buf, int w, int lane, const Map<DIAG> (&mine)[V], Val<DIAG> (&carry)[V],
+                             Val<DIAG> (&into)[V]) {
+    share(buf, w, lane, mine);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+#pragma unroll
+      for (int j = 0; j < S; ++j) {
+        if (j == w) into[v] = carry[v];
+        carry[v] = m[buf][j][v][lane](carry[v]);
       }
     }
   }
-  if (dh0) store_val<DT_F32, DIAG>(dh0, ch.off, a.W, flow);
+};
+
+// Before the carried state is written: it may lie where the first one was
+// read from, by waves that may have had no use for it so far.
+template <int S>
+__device__ __forceinline__ void states_read() {
+  if constexpr (S > 1) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  }
+}
+
+// Workspace of a run cut into segments: slot 0 holds the constant map to the
+// state that enters the first segment, slot g + 1 the map of segment g.
+template <bool DIAG>
+__device__ __forceinline__ Map<DIAG>* slot(void* ws, size_t N, int g) { return static_cast<Map<DIAG>*>(ws) + N * g; }
+
+// The state that enters segment g (the maps of slots 0..g applied in turn):
+// each wave composes a part of the slots, then the waves' maps are exchanged.
+template <bool DIAG, int V, int S>
+__device__ __forceinline__ void enter_segment(void* ws, size_t N, int g, int w, int lane, const Lane<DIAG, V>& l,
+                                              Exchange<DIAG, V, S>& ex, Val<DIAG> (&carry)[V]) {
+  const int per = (g + S) / S, lo = w * per, hi = lo + per < g + 1 ? lo + per : g + 1;
+  Map<DIAG> mine[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) mine[v] = {Val<DIAG>::one(), Val<DIAG>::zero()};
+  for (int i = lo; i < hi; ++i)
+#pragma unroll
+    for (int v = 0; v < V; ++v) mine[v] = slot<DIAG>(ws, N, i)[l.c + v].after(mine[v]);
+  Val<DIAG> into[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) carry[v] = Val<DIAG>::zero();
+  ex(0, w, lane, mine, carry, into);
+}
+
+// Inputs of SCAN_K steps of a wave, [first, end) of them real.
+template <int DT, bool DIAG, int V>
+struct Block {
+  Raw<DT, DIAG, V> u[SCAN_K], g[DIAG ? 1 : SCAN_K];
+  uint8_t done[SCAN_K];  // of the step before
+  __device__ void load(const ScanArgs& a, const Lane<DIAG, V>& l, const void* up, const void* gate,
+                       const uint8_t* dn, int t0, int end) {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) {
+      const int t = t0 + k;
+      if (t < end) {
+        u[k] = load_raw<DT, DIAG, V>(up, l, t, a.W);
+        if constexpr (!DIAG) g[k] = load_raw<DT, DIAG, V>(gate, l, t, a.W);
+        done[k] = 0;
+        if (dn && t > 0) done[k] = dn[(size_t)(t - 1) * a.E + l.env];
+      }
+    }
+  }
+};
+
+template <int DT, bool DIAG, int V>
+__device__ __forceinline__ void load_lambda(const void* gate, const Lane<DIAG, V>& l, int W, Val<DIAG> (&lam)[V]) {
   if constexpr (DIAG) {
-    if (dgate) {
-      dlam_part[ci] = sx;
-      dlam_part[(size_t)N + ci] = sy;
+    const float* f = static_cast<const float*>(gate);
+#pragma unroll
+    for (int v = 0; v < V; ++v) lam[v] = {f[l.p + v], f[W + l.p + v]};
+  }
+}
+
+// Forward.  AGG: fold this segment's steps into its workspace slot; otherwise
+// write h (and, in the last segment, h_last).  seg: steps of a segment.
+template <int DT, bool DIAG, int V, int S, bool AGG>
+__global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u, const void* gate,
+                                                      const uint8_t* done, const float* h0, void* h, float* h_last,
+                                                      void* ws, int seg) {
+  using VT = Val<DIAG>;
+  __shared__ Exchange<DIAG, V, S> ex;
+  const int lane = threadIdx.x & 63, w = S == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lane<DIAG, V> l(a, lane);
+  const size_t N = (size_t)a.E * a.A * a.W;
+  const int g = blockIdx.y;
+  const int first = g * seg, end = a.T - first < seg ? a.T : first + seg;
+  VT lam[V], carry[V], into[V];
+  load_lambda<DT, DIAG, V>(gate, l, a.W, lam);
+  int buf = 0;
+  if (AGG || !ws) {
+    load_state<DIAG, V>(h0, l, a.W, carry);
+    if (AGG && g == 0 && w == 0 && l.live)
+#pragma unroll
+      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
+  } else {
+    enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
+    buf = 1;
+  }
+  Map<DIAG> all[V];  // AGG: everything so far
+#pragma unroll
+  for (int v = 0; v < V; ++v) all[v] = {VT::one(), VT::zero()};
+
+  Block<DT, DIAG, V> cur, nxt;
+  cur.load(a, l, u, gate, done, first + w * SCAN_K, end);
+  for (int t0 = first; t0 < end; t0 += S * SCAN_K) {
+    const int tw = t0 + w * SCAN_K;
+    if (t0 + S * SCAN_K < end) nxt.load(a, l, u, gate, done, tw + S * SCAN_K, end);
+    if constexpr (S > 1) {
+      Map<DIAG> mine[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        VT A = VT::one(), B = VT::zero();
+        bool cut = false;
+#pragma unroll
+        for (int k = 0; k < SCAN_K; ++k)
+          if (tw + k < end) {
+            const VT ak = [&] { if constexpr (DIAG) return lam[v]; else return cur.g[k].get(v); }();
+            const VT uk = cur.u[k].get(v);
+            const bool c = cur.done[k] != 0;
+            B = c ? uk : VT::fma(ak, B, uk);
+            A = VT::mul(ak, A);
+            cut |= c;
+          }
+        mine[v] = folded<DIAG>(A, B, cut);
+      }
+      if constexpr (AGG) {
+        ex.share(buf, w, lane, mine);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int j = 0; j < S; ++j) all[v] = ex.m[buf][j][v][lane].after(all[v]);
+      } else {
+        ex(buf, w, lane, mine, carry, into);
+      }
+      buf ^= 1;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) into[v] = carry[v];
+    }
+    if constexpr (!AGG) {
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k)
+        if (tw + k < end) {
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            const VT ak = [&] { if constexpr (DIAG) return lam[v]; else return cur.g[k].get(v); }();
+            const VT uk = cur.u[k].get(v);
+            into[v] = cur.done[k] != 0 ? uk : VT::fma(ak, into[v], uk);
+          }
+          if (h && l.live) store_vals<DT, DIAG, V>(h, l, tw + k, a.W, into);
+        }
+      if constexpr (S == 1) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) carry[v] = into[v];
+      }
+    }
+    cur = nxt;
+  }
+  if constexpr (AGG) {
+    if (w == 0 && l.live)
+#pragma unroll
+      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, g + 1)[l.c + v] = all[v];
+  } else if (h_last && end == a.T) {
+    states_read<S>();
+    if (w != 0 || !l.live) return;
+    if (done && done[(size_t)(a.T - 1) * a.E + l.env] != 0)
+#pragma unroll
+      for (int v = 0; v < V; ++v) carry[v] = VT::zero();
+    store_state<DIAG, V>(h_last, l, a.W, carry);
+  }
+}
+
+// Backward: steps in falling order (step r of the walk is T - 1 - r), the
+// carried value the gradient that arrives at a step from later ones.  GRAD:
+// the gate's gradient is wanted (h is read).
+template <int DT, bool DIAG, int V, bool GRAD>
+struct BackBlock {
+  Raw<DT, DIAG, V> dh[SCAN_K], g[DIAG ? 1 : SCAN_K], h[GRAD ? SCAN_K : 1];
+  uint8_t done[SCAN_K];  // of the step before (in time)
+  __device__ void load(const ScanArgs& a, const Lane<DIAG, V>& l, const void* dhp, const void* gate, const void* hp,
+                       const uint8_t* dn, int r0, int end) {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) {
+      if (r0 + k < end) {
+        const int t = a.T - 1 - r0 - k;
+        dh[k] = load_raw<DT, DIAG, V>(dhp, l, t, a.W);
+        if constexpr (!DIAG) g[k] = load_raw<DT, DIAG, V>(gate, l, t, a.W);
+        done[k] = 0;
+        if (t > 0) {
+          if constexpr (GRAD) h[k] = load_raw<DT, DIAG, V>(hp, l, t - 1, a.W);
+          if (dn) done[k] = dn[(size_t)(t - 1) * a.E + l.env];
+        }
+      }
+    }
+  }
+};
+
+template <int DT, bool DIAG, int V, int S, bool AGG, bool GRAD>
+__global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void* gate, const uint8_t* done,
+                                                          const float* h0, const void* h, const void* dh,
+                                                          const float* dh_last, void* du, void* dgate, float* dh0,
+                                                          void* ws, double* dlam_part, int seg) {
+  using VT = Val<DIAG>;
+  __shared__ Exchange<DIAG, V, S> ex;
+  const int lane = threadIdx.x & 63, w = S == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lane<DIAG, V> l(a, lane);
+  const size_t N = (size_t)a.E * a.A * a.W;
+  const int g = blockIdx.y;
+  const int first = g * seg, end = a.T - first < seg ? a.T : first + seg;
+  VT lam[V], carry[V], into[V], start[V];
+  load_lambda<DT, DIAG, V>(gate, l, a.W, lam);
+  if constexpr (GRAD) load_state<DIAG, V>(h0, l, a.W, start);
+  int buf = 0;
+  if (AGG || !ws) {
+    const bool ended = done && done[(size_t)(a.T - 1) * a.E + l.env] != 0;
+    load_state<DIAG, V>(ended ? nullptr : dh_last, l, a.W, carry);
+    if (AGG && g == 0 && w == 0 && l.live)
+#pragma unroll
+      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
+  } else {
+    enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
+    buf = 1;
+  }
+  Map<DIAG> all[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) all[v] = {VT::one(), VT::zero()};
+  double sx[V], sy[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) sx[v] = sy[v] = 0.;
+
+  BackBlock<DT, DIAG, V, GRAD> cur, nxt;
+  cur.load(a, l, dh, gate, h, done, first + w * SCAN_K, end);
+  for (int r0 = first; r0 < end; r0 += S * SCAN_K) {
+    const int rw = r0 + w * SCAN_K;
+    if (r0 + S * SCAN_K < end) nxt.load(a, l, dh, gate, h, done, rw + S * SCAN_K, end);
+    if constexpr (S > 1) {
+      Map<DIAG> mine[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        VT A = VT::one(), B = VT::zero();
+        bool cut = false;
+#pragma unroll
+        for (int k = 0; k < SCAN_K; ++k)
+          if (rw + k < end) {
+            const VT ak = [&] { if constexpr (DIAG) return lam[v].conj(); else return cur.g[k].get(v); }();
+            const bool c = cur.done[k] != 0;
+            B = c ? VT::zero() : VT::mul(ak, VT::add(cur.dh[k].get(v), B));
+            A = VT::mul(ak, A);
+            cut |= c;
+          }
+        mine[v] = folded<DIAG>(A, B, cut);
+      }
+      if constexpr (AGG) {
+        ex.share(buf, w, lane, mine);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int j = 0; j < S; ++j) all[v] = ex.m[buf][j][v][lane].after(all[v]);
+      } else {
+        ex(buf, w, lane, mine, carry, into);
+      }
+      buf ^= 1;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) into[v] = carry[v];
+    }
+    if constexpr (!AGG) {
+      float fx[V], fy[V];  // this block's part of the sums over steps
+#pragma unroll
+      for (int v = 0; v < V; ++v) fx[v] = fy[v] = 0.f;
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k)
+        if (rw + k < end) {
+          const int t = a.T - 1 - rw - k;
+          const bool c = cur.done[k] != 0;
+          VT gt[V], dg[V];
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            gt[v] = VT::add(cur.dh[k].get(v), into[v]);
+            const VT ak = [&] { if constexpr (DIAG) return lam[v].conj(); else return cur.g[k].get(v); }();
+            into[v] = c ? VT::zero() : VT::mul(ak, gt[v]);
+            if constexpr (GRAD) {
+              const bool has = !c && (t > 0 || h0);
+              const VT prev = t > 0 ? cur.h[k].get(v) : start[v];
+              dg[v] = has ? VT::mul(gt[v], prev.conj()) : VT::zero();
+              if constexpr (DIAG) {
+                fx[v] += dg[v].x;
+                fy[v] += dg[v].y;
+              }
+            }
+          }
+          if (l.live) {
+            store_vals<DT, DIAG, V>(du, l, t, a.W, gt);
+            if constexpr (GRAD && !DIAG) store_vals<DT, DIAG, V>(dgate, l, t, a.W, dg);
+          }
+        }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if constexpr (S == 1) carry[v] = into[v];
+        if constexpr (GRAD && DIAG) {
+          sx[v] += (double)fx[v];
+          sy[v] += (double)fy[v];
+        }
+      }
+    }
+    cur = nxt;
+  }
+  if constexpr (AGG) {
+    if (w == 0 && l.live)
+#pragma unroll
+      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, g + 1)[l.c + v] = all[v];
+  } else {
+    if (dh0 && end == a.T) {
+      states_read<S>();
+      if (w == 0 && l.live) store_state<DIAG, V>(dh0, l, a.W, carry);
+    }
+    if constexpr (GRAD && DIAG) {
+      // the waves' sums in order, then one partial sum per channel and segment
+      if constexpr (S > 1) {
+        __shared__ double part[S][2][V][64];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          part[w][0][v][lane] = sx[v];
+          part[w][1][v][lane] = sy[v];
+        }
+        __syncthreads();
+        if (w == 0)
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            for (int j = 1; j < S; ++j) {
+              sx[v] += part[j][0][v][lane];
+              sy[v] += part[j][1][v][lane];
+            }
+      }
+      if (w == 0 && l.live)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          dlam_part[(size_t)g * N + l.c + v] = sx[v];
+          dlam_part[(size_t)(gridDim.y + g) * N + l.c + v] = sy[v];
+        }
     }
   }
 }
@@ -169,11 +541,11 @@ __global__ __launch_bounds__(SCAN_NT) void scan_bwd_kernel(ScanArgs a, const voi
 // dlam [2, P]: the partial sums [2, rows, P] added up over the rows, one
 // workgroup per state channel and part.
 constexpr int RED_NT = 256;
-__global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, int rows, int P, float* dlam) {
+__global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, int64_t rows, int P, float* dlam) {
   __shared__ double s[RED_NT];
   const int p = blockIdx.x, c = blockIdx.y;
   double v = 0.;
-  for (int r = threadIdx.x; r < rows; r += RED_NT) v += part[((size_t)c * rows + r) * P + p];
+  for (int64_t r = threadIdx.x; r < rows; r += RED_NT) v += part[(c * rows + r) * P + p];
   s[threadIdx.x] = v;
   __syncthreads();
   for (int d = RED_NT / 2; d > 0; d >>= 1) {
@@ -183,22 +555,99 @@ __global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, i
   if (threadIdx.x == 0) dlam[(size_t)c * P + p] = (float)s[0];
 }
 
+// How a call is split: waves of a workgroup over the steps, and segments.
+struct ScanPlan {
+  int S, G, seg;
+};
+ScanPlan scan_plan(const ScanArgs& p) {
+  const int64_t lanes = (int64_t)p.E * p.A * p.W / (p.dt == DT_BF16 && p.W % 2 == 0 ? 2 : 1);
+  const int64_t waves = (lanes + 63) / 64;
+  ScanPlan s{1, 1, p.T};
+  if (waves >= 4096 || p.T <= 2 * SCAN_K) return s;
+  s.S = SCAN_S;
+  const int block = SCAN_S * SCAN_K;
+  int64_t g = (512 + waves - 1) / waves, most = p.T / (2 * block);
+  if (g > most) g = most;
+  if (g > 1) {
+    s.seg = (int)(((p.T + g - 1) / g + block - 1) / block * block);
+    s.G = (p.T + s.seg - 1) / s.seg;
+  }
+  return s;
+}
+size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t slot_bytes(const ScanArgs& p, const ScanPlan& s) {
+  if (s.G == 1) return 0;
+  return round256((size_t)(s.G + 1) * p.E * p.A * p.W * (p.diag ? sizeof(Map<true>) : sizeof(Map<false>)));
+}
+
+// Two bfloat16 channels to a lane where rows have an even number of them and
+// every array starts at a dword.
+bool pairs(const ScanArgs& p, std::initializer_list<const void*> values) {
+  if (p.dt != DT_BF16 || p.W % 2) return false;
+  for (const void* v : values)
+    if (reinterpret_cast<uintptr_t>(v) & 3) return false;
+  return true;
+}
+
+dim3 scan_grid(const ScanArgs& p, int V, int G) {
+  return dim3((unsigned)(((int64_t)p.E * p.A * p.W / V + 63) / 64), (unsigned)G);
+}
+
+template <int DT, bool DIAG, int V>
+void run_scan(const ScanArgs& p, const ScanPlan& pl, const void* u, const void* gate, const uint8_t* done,
+              const float* h0, void* h, float* h_last, void* ws, hipStream_t s) {
+  if (pl.S == 1) {
+    scan_kernel<DT, DIAG, V, 1, false><<<scan_grid(p, V, 1), 64, 0, s>>>(p, u, gate, done, h0, h, h_last, nullptr, p.T);
+    return;
+  }
+  if (pl.G > 1)
+    scan_kernel<DT, DIAG, V, SCAN_S, true><<<scan_grid(p, V, pl.G - 1), 64 * SCAN_S, 0, s>>>(p, u, gate, done, h0, h,
+                                                                                            h_last, ws, pl.seg);
+  scan_kernel<DT, DIAG, V, SCAN_S, false><<<scan_grid(p, V, pl.G), 64 * SCAN_S, 0, s>>>(
+      p, u, gate, done, h0, h, h_last, pl.G > 1 ? ws : nullptr, pl.seg);
+}
+
+template <int DT, bool DIAG, int V, bool GRAD>
+void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const uint8_t* done, const float* h0,
+                  const void* h, const void* dh, const float* dh_last, void* du, void* dgate, float* dh0, void* ws,
+                  hipStream_t s) {
+  double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + slot_bytes(p, pl));
+  if (pl.S == 1) {
+    scan_bwd_kernel<DT, DIAG, V, 1, false, GRAD><<<scan_grid(p, V, 1), 64, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
+                                                                             dgate, dh0, nullptr, part, p.T);
+  } else {
+    if (pl.G > 1)
+      scan_bwd_kernel<DT, DIAG, V, SCAN_S, true, false><<<scan_grid(p, V, pl.G - 1), 64 * SCAN_S, 0, s>>>(
+          p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, part, pl.seg);
+    scan_bwd_kernel<DT, DIAG, V, SCAN_S, false, GRAD><<<scan_grid(p, V, pl.G), 64 * SCAN_S, 0, s>>>(
+        p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, pl.G > 1 ? ws : nullptr, part, pl.seg);
+  }
+  if (DIAG && GRAD)
+    scan_dlam_kernel<<<dim3((unsigned)p.W, 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
+                                                               static_cast<float*>(dgate));
+}
+
 }  // namespace
 
 size_t scan_workspace_bytes(const ScanArgs& p, bool backward) {
-  return backward && p.diag ? sizeof(double) * 2 * (size_t)p.E * p.A * p.W : 0;
+  const ScanPlan s = scan_plan(p);
+  return slot_bytes(p, s) + (backward && p.diag ? sizeof(double) * 2 * (size_t)s.G * p.E * p.A * p.W : 0);
 }
 
 hipError_t launch_scan(const ScanArgs& p, const void* u, const void* gate, const uint8_t* done, const float* h0,
-                       void* h, float* h_last, void*, hipStream_t s) {
-  const unsigned grid = (unsigned)(((int64_t)p.E * p.A * p.W + SCAN_NT - 1) / SCAN_NT);
-#define RL_SCAN(DT, DIAG) scan_kernel<DT, DIAG><<<grid, SCAN_NT, 0, s>>>(p, u, gate, done, h0, h, h_last)
+                       void* h, float* h_last, void* ws, hipStream_t s) {
+  const ScanPlan pl = scan_plan(p);
+  const bool two = pairs(p, {u, p.diag ? nullptr : gate, h});
+#define RL_SCAN(DT, DIAG, V) run_scan<DT, DIAG, V>(p, pl, u, gate, done, h0, h, h_last, ws, s)
   if (p.dt == DT_F32) {
-    if (p.diag) RL_SCAN(DT_F32, true);
-    else RL_SCAN(DT_F32, false);
+    if (p.diag) RL_SCAN(DT_F32, true, 1);
+    else RL_SCAN(DT_F32, false, 1);
+  } else if (two) {
+    if (p.diag) RL_SCAN(DT_BF16, true, 2);
+    else RL_SCAN(DT_BF16, false, 2);
   } else {
-    if (p.diag) RL_SCAN(DT_BF16, true);
-    else RL_SCAN(DT_BF16, false);
+    if (p.diag) RL_SCAN(DT_BF16, true, 1);
+    else RL_SCAN(DT_BF16, false, 1);
   }
 #undef RL_SCAN
   return hipGetLastError();
@@ -206,21 +655,23 @@ hipError_t launch_scan(const ScanArgs& p, const void* u, const void* gate, const
 
 hipError_t launch_scan_backward(const ScanArgs& p, const void* gate, const uint8_t* done, const float* h0,
                                 const void* h, const void* dh, const float* dh_last, void* du, void* dgate,
-                                float* dh0, void* workspace, hipStream_t s) {
-  const unsigned grid = (unsigned)(((int64_t)p.E * p.A * p.W + SCAN_NT - 1) / SCAN_NT);
-  double* part = static_cast<double*>(workspace);
-#define RL_SCAN(DT, DIAG) \
-  scan_bwd_kernel<DT, DIAG><<<grid, SCAN_NT, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, part)
+                                float* dh0, void* ws, hipStream_t s) {
+  const ScanPlan pl = scan_plan(p);
+  const bool two = pairs(p, {h, dh, du, p.diag ? nullptr : gate, p.diag ? nullptr : dgate});
+#define RL_SCAN(DT, DIAG, V)                                                                                    \
+  (dgate ? run_scan_bwd<DT, DIAG, V, true>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s)        \
+         : run_scan_bwd<DT, DIAG, V, false>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s))
   if (p.dt == DT_F32) {
-    if (p.diag) RL_SCAN(DT_F32, true);
-    else RL_SCAN(DT_F32, false);
+    if (p.diag) RL_SCAN(DT_F32, true, 1);
+    else RL_SCAN(DT_F32, false, 1);
+  } else if (two) {
+    if (p.diag) RL_SCAN(DT_BF16, true, 2);
+    else RL_SCAN(DT_BF16, false, 2);
   } else {
-    if (p.diag) RL_SCAN(DT_BF16, true);
-    else RL_SCAN(DT_BF16, false);
+    if (p.diag) RL_SCAN(DT_BF16, true, 1);
+    else RL_SCAN(DT_BF16, false, 1);
   }
 #undef RL_SCAN
-  if (p.diag && dgate)
-    scan_dlam_kernel<<<dim3((unsigned)p.W, 2), RED_NT, 0, s>>>(part, p.E * p.A, p.W, static_cast<float*>(dgate));
   return hipGetLastError();
 }
 

@@ -33,7 +33,8 @@ def _backward(cfg, gate=_at(0), done=_at(1), h0=_at(2), h=_at(3), dh=_at(4), dh_
 
 
 BAD_SCAN = [(dict(kind=2), R.RL_EUNSUPPORTED), (dict(kind=-1), R.RL_EUNSUPPORTED), (dict(dtype=2), R.RL_EUNSUPPORTED),
-            (dict(n_steps=0), R.RL_EINVAL), (dict(n_envs=0), R.RL_EINVAL), (dict(n_agents=-1), R.RL_EINVAL),
+            (dict(n_steps=0), R.RL_EINVAL), (dict(n_steps=(1 << 30) + 1), R.RL_EINVAL),
+             (dict(n_envs=0), R.RL_EINVAL), (dict(n_agents=-1), R.RL_EINVAL),
             (dict(width=0), R.RL_EINVAL), (dict(n_envs=1 << 20, width=1 << 10), R.RL_EINVAL),
             (dict(n_envs=1 << 30, n_agents=1 << 30, width=1 << 30), R.RL_EINVAL),
             (dict(kind=R.RL_SCAN_DIAGONAL, n_envs=1 << 20, width=1 << 9), R.RL_EINVAL)]
