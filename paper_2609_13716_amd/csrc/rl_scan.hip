@@ -27,7 +27,6 @@ namespace rl {
 namespace {
 
 constexpr int SCAN_K = 8;           // steps a wave holds in registers
-constexpr int SCAN_S = 16;          // waves of a workgroup that split the steps
 constexpr uint32_t SCAN_CUT = 0x7fc0dead;  // a NaN that stands for "the state before is cut off"
 
 // A channel's value: one float, or a complex number.
@@ -555,22 +554,37 @@ __global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, i
   if (threadIdx.x == 0) dlam[(size_t)c * P + p] = (float)s[0];
 }
 
-// How a call is split: waves of a workgroup over the steps, and segments.
+// How a call is split: S waves of a workgroup over the steps, G segments.
+// Measured (one MI355X, us; float32 gates unless said otherwise):
+//   * one wave per 64 channels alone has enough bytes in flight from 2048
+//     waves on (250 steps x 131072 channels: 75 with S = 1, 92 with S = 8; at
+//     65536 channels 46 and 33);
+//   * up to 256 workgroups each has a CU to itself, where 16 waves load more
+//     than 8 (2000 x 16384: 85 against 95); with more of them 8 waves leave
+//     room for a second workgroup (250 x 32768: 19 against 25).  Complex maps
+//     cost more to exchange: 8 is as good or better there at every size;
+//   * segments read the inputs twice, and pay where workgroups leave most CUs
+//     idle (2000 x 4096: 32 in 8 segments, 50 in one; 2000 x 8192: 55 and 55).
 struct ScanPlan {
   int S, G, seg;
 };
 ScanPlan scan_plan(const ScanArgs& p) {
-  const int64_t lanes = (int64_t)p.E * p.A * p.W / (p.dt == DT_BF16 && p.W % 2 == 0 ? 2 : 1);
+  const int64_t lanes = (int64_t)p.E * p.A * p.W / (!p.diag && p.dt == DT_BF16 && p.W % 2 == 0 ? 2 : 1);
   const int64_t waves = (lanes + 63) / 64;
   ScanPlan s{1, 1, p.T};
-  if (waves >= 4096 || p.T <= 2 * SCAN_K) return s;
-  s.S = SCAN_S;
-  const int block = SCAN_S * SCAN_K;
-  int64_t g = (512 + waves - 1) / waves, most = p.T / (2 * block);
-  if (g > most) g = most;
-  if (g > 1) {
+  if (waves >= 2048 || p.T <= 2 * SCAN_K) return s;
+  if (p.T <= 4 * SCAN_K) {
+    s.S = 4;
+    return s;
+  }
+  const int block = 8 * SCAN_K;
+  const int64_t want = (512 + waves - 1) / waves, most = p.T / (2 * block), g = want < most ? want : most;
+  if (waves <= 128 && g >= 4) {
+    s.S = 8;
     s.seg = (int)(((p.T + g - 1) / g + block - 1) / block * block);
     s.G = (p.T + s.seg - 1) / s.seg;
+  } else {
+    s.S = p.diag || waves > 256 || p.T <= block ? 8 : 16;
   }
   return s;
 }
@@ -581,9 +595,11 @@ size_t slot_bytes(const ScanArgs& p, const ScanPlan& s) {
 }
 
 // Two bfloat16 channels to a lane where rows have an even number of them and
-// every array starts at a dword.
+// every array starts at a dword.  Not for complex values: two dwords a step
+// and the wider maps leave room for too few waves (250 steps x 16384 channels:
+// 57 us with pairs, 26 without).
 bool pairs(const ScanArgs& p, std::initializer_list<const void*> values) {
-  if (p.dt != DT_BF16 || p.W % 2) return false;
+  if (p.diag || p.dt != DT_BF16 || p.W % 2) return false;
   for (const void* v : values)
     if (reinterpret_cast<uintptr_t>(v) & 3) return false;
   return true;
@@ -593,39 +609,41 @@ dim3 scan_grid(const ScanArgs& p, int V, int G) {
   return dim3((unsigned)(((int64_t)p.E * p.A * p.W / V + 63) / 64), (unsigned)G);
 }
 
-template <int DT, bool DIAG, int V>
+template <int DT, bool DIAG, int V, int S>
 void run_scan(const ScanArgs& p, const ScanPlan& pl, const void* u, const void* gate, const uint8_t* done,
               const float* h0, void* h, float* h_last, void* ws, hipStream_t s) {
-  if (pl.S == 1) {
-    scan_kernel<DT, DIAG, V, 1, false><<<scan_grid(p, V, 1), 64, 0, s>>>(p, u, gate, done, h0, h, h_last, nullptr, p.T);
-    return;
-  }
-  if (pl.G > 1)
-    scan_kernel<DT, DIAG, V, SCAN_S, true><<<scan_grid(p, V, pl.G - 1), 64 * SCAN_S, 0, s>>>(p, u, gate, done, h0, h,
-                                                                                            h_last, ws, pl.seg);
-  scan_kernel<DT, DIAG, V, SCAN_S, false><<<scan_grid(p, V, pl.G), 64 * SCAN_S, 0, s>>>(
-      p, u, gate, done, h0, h, h_last, pl.G > 1 ? ws : nullptr, pl.seg);
+  if constexpr (S == 8)  // (segments are taken with 8 waves)
+    if (pl.G > 1)
+      scan_kernel<DT, DIAG, V, S, true><<<scan_grid(p, V, pl.G - 1), 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last,
+                                                                                     ws, pl.seg);
+  scan_kernel<DT, DIAG, V, S, false><<<scan_grid(p, V, pl.G), 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last,
+                                                                              pl.G > 1 ? ws : nullptr, pl.seg);
 }
 
-template <int DT, bool DIAG, int V, bool GRAD>
+template <int DT, bool DIAG, int V, int S, bool GRAD>
 void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const uint8_t* done, const float* h0,
                   const void* h, const void* dh, const float* dh_last, void* du, void* dgate, float* dh0, void* ws,
                   hipStream_t s) {
   double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + slot_bytes(p, pl));
-  if (pl.S == 1) {
-    scan_bwd_kernel<DT, DIAG, V, 1, false, GRAD><<<scan_grid(p, V, 1), 64, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
-                                                                             dgate, dh0, nullptr, part, p.T);
-  } else {
+  if constexpr (S == 8)
     if (pl.G > 1)
-      scan_bwd_kernel<DT, DIAG, V, SCAN_S, true, false><<<scan_grid(p, V, pl.G - 1), 64 * SCAN_S, 0, s>>>(
+      scan_bwd_kernel<DT, DIAG, V, S, true, false><<<scan_grid(p, V, pl.G - 1), 64 * S, 0, s>>>(
           p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, part, pl.seg);
-    scan_bwd_kernel<DT, DIAG, V, SCAN_S, false, GRAD><<<scan_grid(p, V, pl.G), 64 * SCAN_S, 0, s>>>(
-        p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, pl.G > 1 ? ws : nullptr, part, pl.seg);
-  }
+  scan_bwd_kernel<DT, DIAG, V, S, false, GRAD><<<scan_grid(p, V, pl.G), 64 * S, 0, s>>>(
+      p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, pl.G > 1 ? ws : nullptr, part, pl.seg);
   if (DIAG && GRAD)
     scan_dlam_kernel<<<dim3((unsigned)p.W, 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
                                                                static_cast<float*>(dgate));
 }
+
+// One of the compiled S.
+#define RL_SCAN(DT, DIAG, V)             \
+  switch (pl.S) {                        \
+    case 1: RL_SCAN_S(DT, DIAG, V, 1); break;   \
+    case 4: RL_SCAN_S(DT, DIAG, V, 4); break;   \
+    case 8: RL_SCAN_S(DT, DIAG, V, 8); break;   \
+    default: RL_SCAN_S(DT, DIAG, V, 16); break; \
+  }
 
 }  // namespace
 
@@ -637,19 +655,16 @@ size_t scan_workspace_bytes(const ScanArgs& p, bool backward) {
 hipError_t launch_scan(const ScanArgs& p, const void* u, const void* gate, const uint8_t* done, const float* h0,
                        void* h, float* h_last, void* ws, hipStream_t s) {
   const ScanPlan pl = scan_plan(p);
-  const bool two = pairs(p, {u, p.diag ? nullptr : gate, h});
-#define RL_SCAN(DT, DIAG, V) run_scan<DT, DIAG, V>(p, pl, u, gate, done, h0, h, h_last, ws, s)
+  const bool two = pairs(p, {u, gate, h});
+#define RL_SCAN_S(DT, DIAG, V, S) run_scan<DT, DIAG, V, S>(p, pl, u, gate, done, h0, h, h_last, ws, s)
   if (p.dt == DT_F32) {
-    if (p.diag) RL_SCAN(DT_F32, true, 1);
-    else RL_SCAN(DT_F32, false, 1);
+    if (p.diag) RL_SCAN(DT_F32, true, 1) else RL_SCAN(DT_F32, false, 1)
   } else if (two) {
-    if (p.diag) RL_SCAN(DT_BF16, true, 2);
-    else RL_SCAN(DT_BF16, false, 2);
+    RL_SCAN(DT_BF16, false, 2)
   } else {
-    if (p.diag) RL_SCAN(DT_BF16, true, 1);
-    else RL_SCAN(DT_BF16, false, 1);
+    if (p.diag) RL_SCAN(DT_BF16, true, 1) else RL_SCAN(DT_BF16, false, 1)
   }
-#undef RL_SCAN
+#undef RL_SCAN_S
   return hipGetLastError();
 }
 
@@ -657,21 +672,18 @@ hipError_t launch_scan_backward(const ScanArgs& p, const void* gate, const uint8
                                 const void* h, const void* dh, const float* dh_last, void* du, void* dgate,
                                 float* dh0, void* ws, hipStream_t s) {
   const ScanPlan pl = scan_plan(p);
-  const bool two = pairs(p, {h, dh, du, p.diag ? nullptr : gate, p.diag ? nullptr : dgate});
-#define RL_SCAN(DT, DIAG, V)                                                                                    \
-  (dgate ? run_scan_bwd<DT, DIAG, V, true>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s)        \
-         : run_scan_bwd<DT, DIAG, V, false>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s))
+  const bool two = pairs(p, {h, dh, du, gate, dgate});
+#define RL_SCAN_S(DT, DIAG, V, S)                                                                               \
+  (dgate ? run_scan_bwd<DT, DIAG, V, S, true>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s)     \
+         : run_scan_bwd<DT, DIAG, V, S, false>(p, pl, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, s))
   if (p.dt == DT_F32) {
-    if (p.diag) RL_SCAN(DT_F32, true, 1);
-    else RL_SCAN(DT_F32, false, 1);
+    if (p.diag) RL_SCAN(DT_F32, true, 1) else RL_SCAN(DT_F32, false, 1)
   } else if (two) {
-    if (p.diag) RL_SCAN(DT_BF16, true, 2);
-    else RL_SCAN(DT_BF16, false, 2);
+    RL_SCAN(DT_BF16, false, 2)
   } else {
-    if (p.diag) RL_SCAN(DT_BF16, true, 1);
-    else RL_SCAN(DT_BF16, false, 1);
+    if (p.diag) RL_SCAN(DT_BF16, true, 1) else RL_SCAN(DT_BF16, false, 1)
   }
-#undef RL_SCAN
+#undef RL_SCAN_S
   return hipGetLastError();
 }
 
