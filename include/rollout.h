@@ -342,7 +342,8 @@ typedef struct {
   float entropy_coef;    /* finite */
 } rl_ppo_config;
 
-/* Bytes of workspace rl_ppo_loss needs; 0 if the config is invalid. */
+/* Bytes of workspace rl_ppo_loss needs; 0 when it needs none (few rows) or the
+ * config is invalid. */
 size_t rl_ppo_workspace_bytes(const rl_ppo_config* cfg);
 
 /*   logits [R, nA] float32, legal [R, nA] uint8 or NULL (all legal), mask [R]

@@ -658,7 +658,7 @@ rl_status rl_ppo_loss(const rl_ppo_config* cfg, const float* logits, const uint8
   for (const void* w : words)
     if (!aligned_to(w, 4)) return fail(RL_EINVAL, "an array is not aligned to its elements");
   const size_t need = rl::ppo_workspace_bytes(cfg->n_rows);
-  if (!workspace || !aligned16(workspace) || workspace_bytes < need)
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
     return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
   const rl::PpoArgs p{cfg->n_rows, cfg->n_actions, cfg->normalize_adv, cfg->clip, cfg->value_clip, cfg->value_coef,
                       cfg->entropy_coef, logits, legal, mask, actions, logp_old, adv, value,

@@ -537,21 +537,23 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
   }
 }
 
-// dlam [2, P]: the partial sums [2, rows, P] added up over the rows, one
-// workgroup per state channel and part.
-constexpr int RED_NT = 256;
+// dlam [2, P]: the partial sums [2, rows, P] added up over the rows.  A
+// workgroup takes RED_P neighbouring channels (64 bytes of a row) and
+// RED_NT / RED_P rows at a time.
+constexpr int RED_NT = 1024, RED_P = 8;
 __global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, int64_t rows, int P, float* dlam) {
   __shared__ double s[RED_NT];
-  const int p = blockIdx.x, c = blockIdx.y;
+  const int tid = threadIdx.x, p = blockIdx.x * RED_P + tid % RED_P, c = blockIdx.y;
   double v = 0.;
-  for (int64_t r = threadIdx.x; r < rows; r += RED_NT) v += part[(c * rows + r) * P + p];
-  s[threadIdx.x] = v;
+  if (p < P)
+    for (int64_t r = tid / RED_P; r < rows; r += RED_NT / RED_P) v += part[(c * rows + r) * P + p];
+  s[tid] = v;
   __syncthreads();
-  for (int d = RED_NT / 2; d > 0; d >>= 1) {
-    if (threadIdx.x < d) s[threadIdx.x] += s[threadIdx.x + d];
+  for (int d = RED_NT / 2; d >= RED_P; d >>= 1) {
+    if (tid < d) s[tid] += s[tid + d];
     __syncthreads();
   }
-  if (threadIdx.x == 0) dlam[(size_t)c * P + p] = (float)s[0];
+  if (tid < RED_P && p < P) dlam[(size_t)c * P + p] = (float)s[tid];
 }
 
 // How a call is split: S waves of a workgroup over the steps, G segments.
@@ -632,7 +634,7 @@ void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const
   scan_bwd_kernel<DT, DIAG, V, S, false, GRAD><<<scan_grid(p, V, pl.G), 64 * S, 0, s>>>(
       p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, pl.G > 1 ? ws : nullptr, part, pl.seg);
   if (DIAG && GRAD)
-    scan_dlam_kernel<<<dim3((unsigned)p.W, 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
+    scan_dlam_kernel<<<dim3((unsigned)((p.W + RED_P - 1) / RED_P), 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
                                                                static_cast<float*>(dgate));
 }
 

@@ -9,7 +9,9 @@ and streams.  The library must have been built
 loudly otherwise -- there is no fallback path.
 """
 
+import contextlib
 import ctypes
+import functools
 import os
 from dataclasses import dataclass, field
 
@@ -597,73 +599,94 @@ def gae(reward, done, value, value_last, gamma, lam, adv=None, ret=None, stream=
 # ---- a learner's operators (see the learner section of include/rollout.h) ----
 
 
-class _On:
-    """Where a learner's call runs: the device its tensors share, and the stream given or that device's current one.
-    Inside the block both are torch's current ones, so what the call allocates belongs to that stream."""
-
-    def __init__(self, stream, **tensors):
-        dev = None
-        for name, t in tensors.items():
-            if t is None:
-                continue
-            if not t.is_cuda:
-                raise ValueError(f"{name} must be a device tensor")
-            if dev is None:
-                dev = t.device
-            elif t.device != dev:
-                raise ValueError(f"{name} is on {t.device}, the tensors before it on {dev}")
-        if stream is not None and stream.device != dev:
-            raise ValueError(f"the stream is on {stream.device}, the tensors are on {dev}")
-        self._guards = []
-        if dev.index != torch.cuda.current_device():
-            self._guards.append(torch.cuda.device(dev))
-        if stream is not None:
-            self._guards.append(torch.cuda.stream(stream))
-
-    def __enter__(self):
-        for g in self._guards:
-            g.__enter__()
-
-    def __exit__(self, *exc):
-        for g in reversed(self._guards):
-            g.__exit__(*exc)
+def _lead(t, name):
+    """The device index of a call's first tensor."""
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    return dev
 
 
-def _new(t, shape, dtype, like):
-    return torch.empty(shape, dtype=dtype, device=like.device) if t is None else t
+def _arg(t, name, dtype, shape, dev):
+    """The address of a tensor argument (None for None), checked: on the call's device, contiguous, of that dtype and
+    shape."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be a device tensor" if not t.is_cuda else
+                         f"{name} is on {t.device}, the call's first tensor on cuda:{dev}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _workspace(workspace, nbytes, like):
-    """(tensor or None, its bytes) for a call that needs nbytes; allocated when not given."""
+def _on(stream, dev):
+    """A context in which torch's current device and stream are the call's: the device its tensors are on, and the
+    stream given or that device's current one.  What the call allocates inside belongs to that stream."""
+    if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors are on cuda:{dev}")
+        return torch.cuda.stream(stream)  # (switches to the stream's device, too)
+    return _HERE_ALREADY if torch.cuda.current_device() == dev else torch.cuda.device(dev)
+
+
+# The current stream's handle of a device.  torch.cuda.current_stream(dev).cuda_stream is the same through an object that
+# takes 2.6 us to make, a third of what a call of one small step takes in all.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _workspace(workspace, nbytes, dev):
+    """(tensor to keep until the call is made, its address, its bytes) for a call that needs nbytes; allocated when
+    not given."""
     if workspace is None:
         if nbytes == 0:
-            return None, 0
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    else:
-        _need(workspace, "workspace", torch.uint8)
-    return workspace, workspace.numel()
+            return None, None, 0
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+    n = workspace.numel()
+    return workspace, _arg(workspace, "workspace", torch.uint8, (n,), dev), n
 
 
-def _scan_config(values, gate, name):
-    """The C config, and the shapes of the states and of the gate, for values [T, E, A, D] (gated) or
-    [T, E, A, 2, P] (diagonal: gate is lambda_bar [2, P])."""
-    if values.dtype not in _DT_CODE:
+class _Sizes:
+    """A call's C config and the workspace it needs; they follow from its sizes alone."""
+    __slots__ = ("cfg", "ref", "need", "need_backward")
+
+
+@functools.lru_cache(maxsize=1024)
+def _scan_sizes(kind, dtype, T, E, A, W):
+    z = _Sizes()
+    if max(T, E, A, W) > 0x7fffffff:
+        raise ValueError(f"a size is beyond 32 bits: {(T, E, A, W)}")
+    z.cfg = _ScanConfig(kind, dtype, T, E, A, W)
+    z.ref = ctypes.byref(z.cfg)
+    z.need, z.need_backward = lib.rl_scan_workspace_bytes(z.ref, 0), lib.rl_scan_workspace_bytes(z.ref, 1)
+    return z
+
+
+def _scan_shapes(values, gate, name):
+    """(sizes, the gate's dtype and shape) for values [T, E, A, D] (gated) or [T, E, A, 2, P] (diagonal: gate is
+    lambda_bar [2, P])."""
+    code = _DT_CODE.get(values.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32 or bfloat16, got {values.dtype}")
-    s = tuple(values.shape)
-    diag = gate.dim() == 2
-    if len(s) != (5 if diag else 4) or (diag and s[3] != 2):
-        raise ValueError(f"{name} must be " + ("[T, E, A, 2, P] (the gate is [2, P])" if diag else "[T, E, A, D]") +
-                         f", got {s}")
-    if max(s) > 0x7fffffff:
-        raise ValueError(f"{name} has a size beyond 32 bits: {s}")
-    cfg = _ScanConfig(RL_SCAN_DIAGONAL if diag else RL_SCAN_GATED, _DT_CODE[values.dtype], s[0], s[1], s[2], s[-1])
-    return cfg, (2, s[4]) if diag else s
+    s = values.shape
+    if gate.dim() == 2:
+        if len(s) != 5 or s[3] != 2:
+            raise ValueError(f"{name} must be [T, E, A, 2, P] (the gate is [2, P]), got {tuple(s)}")
+        return _scan_sizes(RL_SCAN_DIAGONAL, code, s[0], s[1], s[2], s[4]), torch.float32, (2, s[4])
+    if len(s) != 4:
+        raise ValueError(f"{name} must be [T, E, A, D], got {tuple(s)}")
+    return _scan_sizes(RL_SCAN_GATED, code, s[0], s[1], s[2], s[3]), values.dtype, s
 
 
 def scan_workspace_bytes(values, gate, backward=False):
     """Bytes of workspace scan (or scan_backward) needs for values and a gate of these shapes."""
-    cfg, _ = _scan_config(values, gate, "values")
-    return lib.rl_scan_workspace_bytes(ctypes.byref(cfg), int(backward))
+    z = _scan_shapes(values, gate, "values")[0]
+    return z.need_backward if backward else z.need
 
 
 def scan(u, gate, done=None, h0=None, h=None, h_last=None, workspace=None, stream=None):
@@ -673,20 +696,19 @@ def scan(u, gate, done=None, h0=None, h=None, h_last=None, workspace=None, strea
     h0 float32, one step's shape.  Returns (h, h_last): the states, and the float32 state the next call starts from
     (h_last may be h0: the state is advanced in place).  ``workspace``: a uint8 tensor of at least
     scan_workspace_bytes(u, gate) bytes (allocated when None)."""
-    cfg, gshape = _scan_config(u, gate, "u")
-    T, E, state = u.shape[0], u.shape[1], u.shape[1:]
-    _need(u, "u")
-    _need(gate, "gate", torch.float32 if cfg.kind == RL_SCAN_DIAGONAL else u.dtype, gshape)
-    _need(done, "done", torch.uint8, (T, E))
-    _need(h0, "h0", torch.float32, state)
-    with _On(stream, u=u, gate=gate, done=done, h0=h0, h=h, h_last=h_last, workspace=workspace):
-        h, h_last = _new(h, u.shape, u.dtype, u), _new(h_last, state, torch.float32, u)
-        _need(h, "h", u.dtype, u.shape)
-        _need(h_last, "h_last", torch.float32, state)
-        c = ctypes.byref(cfg)
-        ws, n = _workspace(workspace, lib.rl_scan_workspace_bytes(c, 0), u)
-        _check(lib.rl_scan(c, _ptr(u), _ptr(gate), _ptr(done), _ptr(h0), _ptr(h), _ptr(h_last), _ptr(ws), n,
-                           _stream()))
+    z, gate_dtype, gate_shape = _scan_shapes(u, gate, "u")
+    dev, dt, shape = _lead(u, "u"), u.dtype, u.shape
+    state, f32 = shape[1:], torch.float32
+    with _on(stream, dev):
+        if h is None:
+            h = torch.empty(shape, dtype=dt, device=dev)
+        if h_last is None:
+            h_last = torch.empty(state, dtype=f32, device=dev)
+        args = (_arg(u, "u", dt, shape, dev), _arg(gate, "gate", gate_dtype, gate_shape, dev),
+                _arg(done, "done", torch.uint8, shape[:2], dev), _arg(h0, "h0", f32, state, dev),
+                _arg(h, "h", dt, shape, dev), _arg(h_last, "h_last", f32, state, dev))
+        keep, ws, n = _workspace(workspace, z.need, dev)
+        _check(lib.rl_scan(z.ref, *args, ws, n, _raw_stream(dev)))
     return h, h_last
 
 
@@ -695,26 +717,22 @@ def scan_backward(gate, h, dh, done=None, h0=None, dh_last=None, du=None, dgate=
     """Gradients of scan: from dh (of its h) and dh_last (of its h_last, None: zeros), with gate, done and h0 as given
     to it and h as it returned it.  Returns (du, dgate, dh0); see rl_scan_backward in include/rollout.h.
     dh0 may be dh_last.  ``workspace``: at least scan_workspace_bytes(dh, gate, True) bytes (allocated when None)."""
-    cfg, gshape = _scan_config(dh, gate, "dh")
-    T, E, state = dh.shape[0], dh.shape[1], dh.shape[1:]
-    gdt = torch.float32 if cfg.kind == RL_SCAN_DIAGONAL else dh.dtype
-    _need(dh, "dh")
-    _need(h, "h", dh.dtype, dh.shape)
-    _need(gate, "gate", gdt, gshape)
-    _need(done, "done", torch.uint8, (T, E))
-    _need(h0, "h0", torch.float32, state)
-    _need(dh_last, "dh_last", torch.float32, state)
-    with _On(stream, dh=dh, gate=gate, h=h, done=done, h0=h0, dh_last=dh_last, du=du, dgate=dgate, dh0=dh0,
-             workspace=workspace):
-        du, dgate = _new(du, dh.shape, dh.dtype, dh), _new(dgate, gshape, gdt, dh)
-        dh0 = _new(dh0, state, torch.float32, dh)
-        _need(du, "du", dh.dtype, dh.shape)
-        _need(dgate, "dgate", gdt, gshape)
-        _need(dh0, "dh0", torch.float32, state)
-        c = ctypes.byref(cfg)
-        ws, n = _workspace(workspace, lib.rl_scan_workspace_bytes(c, 1), dh)
-        _check(lib.rl_scan_backward(c, _ptr(gate), _ptr(done), _ptr(h0), _ptr(h), _ptr(dh), _ptr(dh_last), _ptr(du),
-                                    _ptr(dgate), _ptr(dh0), _ptr(ws), n, _stream()))
+    z, gate_dtype, gate_shape = _scan_shapes(dh, gate, "dh")
+    dev, dt, shape = _lead(dh, "dh"), dh.dtype, dh.shape
+    state, f32 = shape[1:], torch.float32
+    with _on(stream, dev):
+        if du is None:
+            du = torch.empty(shape, dtype=dt, device=dev)
+        if dgate is None:
+            dgate = torch.empty(gate_shape, dtype=gate_dtype, device=dev)
+        if dh0 is None:
+            dh0 = torch.empty(state, dtype=f32, device=dev)
+        args = (_arg(gate, "gate", gate_dtype, gate_shape, dev), _arg(done, "done", torch.uint8, shape[:2], dev),
+                _arg(h0, "h0", f32, state, dev), _arg(h, "h", dt, shape, dev), _arg(dh, "dh", dt, shape, dev),
+                _arg(dh_last, "dh_last", f32, state, dev), _arg(du, "du", dt, shape, dev),
+                _arg(dgate, "dgate", gate_dtype, gate_shape, dev), _arg(dh0, "dh0", f32, state, dev))
+        keep, ws, n = _workspace(workspace, z.need_backward, dev)
+        _check(lib.rl_scan_backward(z.ref, *args, ws, n, _raw_stream(dev)))
     return du, dgate, dh0
 
 
@@ -730,42 +748,43 @@ def ppo_loss(logits, actions, logp_old, adv, value, ret, clip=0.2, value_coef=0.
     and value_old float32 and mask uint8 of that leading shape, legal uint8 like logits.  Returns (dlogits, dvalue,
     stats), stats [6] named by PPO_STATS.  ``workspace``: uint8, at least ppo_workspace_bytes(logits) bytes
     (allocated when None)."""
-    lead, na = tuple(logits.shape[:-1]), logits.shape[-1]
-    _need(logits, "logits", torch.float32)
-    _need(actions, "actions", torch.int32, lead)
-    for name, t in (("logp_old", logp_old), ("adv", adv), ("value", value), ("ret", ret), ("value_old", value_old)):
-        _need(t, name, torch.float32, lead)
-    _need(legal, "legal", torch.uint8, logits.shape)
-    _need(mask, "mask", torch.uint8, lead)
-    cfg = _PpoConfig(value.numel(), na, int(normalize), clip, value_clip, value_coef, entropy_coef)
-    with _On(stream, logits=logits, actions=actions, logp_old=logp_old, adv=adv, value=value, ret=ret,
-             value_old=value_old, legal=legal, mask=mask, dlogits=dlogits, dvalue=dvalue, stats=stats,
-             workspace=workspace):
-        dlogits, dvalue = _new(dlogits, logits.shape, torch.float32, logits), _new(dvalue, lead, torch.float32, logits)
-        stats = _new(stats, (6,), torch.float32, logits)
-        _need(dlogits, "dlogits", torch.float32, logits.shape)
-        _need(dvalue, "dvalue", torch.float32, lead)
-        _need(stats, "stats", torch.float32, (6,))
-        c = ctypes.byref(cfg)
-        ws, n = _workspace(workspace, lib.rl_ppo_workspace_bytes(c), logits)
-        _check(lib.rl_ppo_loss(c, _ptr(logits), _ptr(legal), _ptr(mask), _ptr(actions), _ptr(logp_old), _ptr(adv),
-                               _ptr(value), _ptr(value_old), _ptr(ret), _ptr(dlogits), _ptr(dvalue), _ptr(stats),
-                               _ptr(ws), n, _stream()))
+    dev, shape = _lead(logits, "logits"), logits.shape
+    lead, na = shape[:-1], shape[-1]
+    f32, u8 = torch.float32, torch.uint8
+    cfg = _PpoConfig(lead.numel(), na, int(normalize), clip, value_clip, value_coef, entropy_coef)
+    ref = ctypes.byref(cfg)
+    with _on(stream, dev):
+        if dlogits is None:
+            dlogits = torch.empty(shape, dtype=f32, device=dev)
+        if dvalue is None:
+            dvalue = torch.empty(lead, dtype=f32, device=dev)
+        if stats is None:
+            stats = torch.empty(6, dtype=f32, device=dev)
+        args = (_arg(logits, "logits", f32, shape, dev), _arg(legal, "legal", u8, shape, dev),
+                _arg(mask, "mask", u8, lead, dev), _arg(actions, "actions", torch.int32, lead, dev),
+                _arg(logp_old, "logp_old", f32, lead, dev), _arg(adv, "adv", f32, lead, dev),
+                _arg(value, "value", f32, lead, dev), _arg(value_old, "value_old", f32, lead, dev),
+                _arg(ret, "ret", f32, lead, dev), _arg(dlogits, "dlogits", f32, shape, dev),
+                _arg(dvalue, "dvalue", f32, lead, dev), _arg(stats, "stats", f32, (6,), dev))
+        keep, ws, n = _workspace(workspace, lib.rl_ppo_workspace_bytes(ref), dev)
+        _check(lib.rl_ppo_loss(ref, *args, ws, n, _raw_stream(dev)))
     return dlogits, dvalue, stats
 
 
 def ppo_workspace_bytes(logits):
     """Bytes of workspace ppo_loss needs for these logits."""
-    cfg = _PpoConfig(logits.numel() // max(logits.shape[-1], 1), logits.shape[-1], 0, 0.2, 0.0, 0.0, 0.0)
+    cfg = _PpoConfig(logits.shape[:-1].numel(), logits.shape[-1], 0, 0.2, 0.0, 0.0, 0.0)
     return lib.rl_ppo_workspace_bytes(ctypes.byref(cfg))
 
 
 def _ortho_sizes(g):
-    if g.dtype not in _DT_CODE:
+    code = _DT_CODE.get(g.dtype)
+    if code is None:
         raise ValueError(f"g must be float32 or bfloat16, got {g.dtype}")
     if g.dim() not in (2, 3):
         raise ValueError(f"g must be [rows, cols] or [n, rows, cols], got {tuple(g.shape)}")
-    return (g.shape[0] if g.dim() == 3 else 1), g.shape[-2], g.shape[-1], _DT_CODE[g.dtype]
+    s = g.shape
+    return (s[0] if len(s) == 3 else 1), s[-2], s[-1], code
 
 
 def orthogonalize_workspace_bytes(g):
@@ -778,12 +797,13 @@ def orthogonalize(g, steps=5, out=None, workspace=None, stream=None):
     float32 or bfloat16); out may be g.  See rl_orthogonalize in include/rollout.h.  ``workspace``: uint8, at least
     orthogonalize_workspace_bytes(g) bytes (allocated when None)."""
     sizes = _ortho_sizes(g)
-    _need(g, "g")
-    with _On(stream, g=g, out=out, workspace=workspace):
-        out = _new(out, g.shape, g.dtype, g)
-        _need(out, "out", g.dtype, g.shape)
-        ws, n = _workspace(workspace, lib.rl_orthogonalize_workspace_bytes(*sizes), g)
-        _check(lib.rl_orthogonalize(*sizes, steps, _ptr(g), _ptr(out), _ptr(ws), n, _stream()))
+    dev, dt, shape = _lead(g, "g"), g.dtype, g.shape
+    with _on(stream, dev):
+        if out is None:
+            out = torch.empty(shape, dtype=dt, device=dev)
+        args = _arg(g, "g", dt, shape, dev), _arg(out, "out", dt, shape, dev)
+        keep, ws, n = _workspace(workspace, lib.rl_orthogonalize_workspace_bytes(*sizes), dev)
+        _check(lib.rl_orthogonalize(*sizes, steps, *args, ws, n, _raw_stream(dev)))
     return out
 
 

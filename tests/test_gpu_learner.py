@@ -238,8 +238,7 @@ def test_scan_optional_arguments(kind):
         carry = s.h0.clone()
         h2, l2 = R.scan(s.u, s.gate, s.done, carry, h_last=carry)
         assert l2 is carry and torch.equal(h2, h) and torch.equal(carry, last)
-        cfg, _ = R._scan_config(s.u, s.gate, "u")
-        c = R.ctypes.byref(cfg)
+        c = R._scan_shapes(s.u, s.gate, "u")[0].ref
         ws = torch.empty(max(R.scan_workspace_bytes(s.u, s.gate), R.scan_workspace_bytes(s.u, s.gate, True), 1),
                          dtype=torch.uint8, device="cuda")
         st, p = R._stream(), R._ptr

@@ -75,7 +75,7 @@ def test_scan_workspace():
 
 
 def _ppo_cfg(**kw):
-    v = dict(n_rows=100, n_actions=6, normalize_adv=1, clip=0.2, value_clip=0.2, value_coef=0.5, entropy_coef=0.01)
+    v = dict(n_rows=20000, n_actions=6, normalize_adv=1, clip=0.2, value_clip=0.2, value_coef=0.5, entropy_coef=0.01)
     v.update(kw)
     return R._PpoConfig(**v)
 
