@@ -39,7 +39,7 @@ __device__ __forceinline__ void split8(const float (&v)[8], f16x8* hi, f16x8* lo
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     h[e] = (_Float16)v[e];
-    l[e] = (_Float16)((v[e] - (float)h[e]) * LO_SCALE);
+    l[e] = (_Float16)fmaf(-LO_SCALE, (float)h[e], LO_SCALE * v[e]);  // (exact before it is rounded)
   }
   *hi = h;
   *lo = l;
@@ -203,22 +203,29 @@ __device__ __forceinline__ void acc_to_lds(const f32x16& acc, const f32x16& low,
 // What a product's value v (4 of a row: row i, columns j.. of the tile at i0,
 // j0) becomes: B from A A, or the new X, which is stored in float32, too.
 template <int MODE>
-__device__ __forceinline__ f32x4 finish4(const NsArgs& p, size_t mat, int i0, int j0, int i, int j, f32x4 v) {
-  if constexpr (MODE == NS_POLY) {
-    const _Float16* a = p.a + mat * p.mp * p.mp * 2 + ((size_t)(i0 / 32) * (p.mp / 16) + (j0 + j) / 16) * BLOCK +
-                        (i + 32 * (((j0 + j) & 15) / 8)) * 8 + (j & 7);
+struct Finish {
+  f32x4 old;  // A's or X's values of the same places
+  __device__ void load(const NsArgs& p, size_t mat, int i0, int j0, int i, int j) {
+    if constexpr (MODE == NS_POLY) {
+      const _Float16* a = p.a + mat * p.mp * p.mp * 2 + ((size_t)(i0 / 32) * (p.mp / 16) + (j0 + j) / 16) * BLOCK +
+                          (i + 32 * (((j0 + j) & 15) / 8)) * 8 + (j & 7);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = NS_C * v[e] + NS_B * ((float)a[e] + (float)a[512 + e] * (1.f / LO_SCALE));
+      for (int e = 0; e < 4; ++e) old[e] = (float)a[e] + (float)a[512 + e] * (1.f / LO_SCALE);
+    }
+    if constexpr (MODE == NS_STEP || MODE == NS_LAST)
+      old = *reinterpret_cast<const f32x4*>(p.xf + mat * p.mp * p.kp + (size_t)(i0 + i) * p.kp + j0 + j);
   }
-  if constexpr (MODE == NS_STEP || MODE == NS_LAST) {
-    f32x4* x = reinterpret_cast<f32x4*>(p.xf + mat * p.mp * p.kp + (size_t)(i0 + i) * p.kp + j0 + j);
-    const f32x4 old = *x;
+  __device__ f32x4 operator()(const NsArgs& p, size_t mat, int i0, int j0, int i, int j, f32x4 v) const {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(NS_A, old[e], v[e]);
-    if constexpr (MODE == NS_STEP) *x = v;
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (MODE == NS_POLY) v[e] = NS_C * v[e] + NS_B * old[e];
+      if constexpr (MODE == NS_STEP || MODE == NS_LAST) v[e] = fmaf(NS_A, old[e], v[e]);
+    }
+    if constexpr (MODE == NS_STEP)
+      *reinterpret_cast<f32x4*>(p.xf + mat * p.mp * p.kp + (size_t)(i0 + i) * p.kp + j0 + j) = v;
+    return v;
   }
-  return v;
-}
+};
 
 // The finished tile in LDS -> its operands, or the caller's matrix.
 template <int MODE, int DT>
@@ -271,6 +278,9 @@ __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles)
   const _Float16* P = op.P + (size_t)ti * op.steps * BLOCK + lane * 8;
   const _Float16* Q = op.Q + (size_t)tj * op.steps * BLOCK + lane * 8;
   const int per = (op.steps + NS_W - 1) / NS_W, lo = w * per, hi = lo + per < op.steps ? lo + per : op.steps;
+  const int i0 = ti * TS, j0 = tj * TS, i = tid >> 3, j = (tid & 7) * 4;
+  Finish<MODE> fin;
+  fin.load(p, mat, i0, j0, i, j);  // (early: it arrives while the products run)
   f32x16 acc = {}, low = {};
   f16x8 a[NS_AHEAD][2], b[NS_AHEAD][2];
 #pragma unroll
@@ -292,11 +302,10 @@ __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles)
   }
   acc_to_lds(acc, low, s[w], lane);
   __syncthreads();
-  const int i0 = ti * TS, j0 = tj * TS, i = tid >> 3, j = (tid & 7) * 4;
   f32x4 v = *reinterpret_cast<const f32x4*>(&s[0][i * LDT + j]);
 #pragma unroll
   for (int q = 1; q < NS_W; ++q) v += *reinterpret_cast<const f32x4*>(&s[q][i * LDT + j]);
-  *reinterpret_cast<f32x4*>(&s[0][i * LDT + j]) = finish4<MODE>(p, mat, i0, j0, i, j, v);
+  *reinterpret_cast<f32x4*>(&s[0][i * LDT + j]) = fin(p, mat, i0, j0, i, j, v);
   __syncthreads();
   put_tile<MODE, DT>(p, mat, i0, j0, s[0], tid, 64 * NS_W);
 }
@@ -306,7 +315,7 @@ __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles)
 // every operand block is read by two of them and the second read meets it in
 // the L1 cache.  Two-dimensional sizes are padded to 128.
 constexpr int WIDE = 128;
-constexpr int WIDE_AHEAD = 4;  // (steps are multiples of 8)
+constexpr int WIDE_AHEAD = 8;  // (steps are multiples of it)
 
 template <int MODE, int DT>
 __global__ __launch_bounds__(256, 1) void ns_wide_kernel(NsArgs p, int tiles) {
@@ -352,18 +361,342 @@ __global__ __launch_bounds__(256, 1) void ns_wide_kernel(NsArgs p, int tiles) {
     for (int y = 0; y < 2; ++y) {
       const int i0 = (ti + x) * TS, j0 = (tj + y) * TS;
       if ((MODE == NS_GRAM || MODE == NS_POLY) && j0 > i0) continue;
+      Finish<MODE> fin[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) fin[u].load(p, mat, i0, j0, (lane + u * 64) >> 3, (lane & 7) * 4);
       acc_to_lds(acc[x][y], low[x][y], s[w], lane);
       wave_lds_sync();
 #pragma unroll
-      for (int c = lane; c < TS * TS / 4; c += 64) {
-        f32x4* v = reinterpret_cast<f32x4*>(&s[w][(c >> 3) * LDT + (c & 7) * 4]);
-        *v = finish4<MODE>(p, mat, i0, j0, c >> 3, (c & 7) * 4, *v);
+      for (int u = 0; u < 4; ++u) {
+        const int i = (lane + u * 64) >> 3, j = (lane & 7) * 4;
+        f32x4* v = reinterpret_cast<f32x4*>(&s[w][i * LDT + j]);
+        *v = fin[u](p, mat, i0, j0, i, j, *v);
       }
       wave_lds_sync();
       put_tile<MODE, DT>(p, mat, i0, j0, s[w], lane, 64);
       wave_lds_sync();
     }
 }
+
+// ---- one workgroup per matrix ----
+//
+// Matrices whose X fits in one CU (policy layers): all steps in one launch.
+// X lives in registers, in the layout that the 16 x 16 x 32 matrix instruction
+// writes: a wave owns NS strips of 16 columns, all rows (lane l: column l % 16,
+// rows 16 it + 4 (l / 16) ..+3).  That is also the layout in which it reads X
+// for B X, when the sum over rows takes them in the order (tile 2s: 4 rows of
+// the lane's group, tile 2s + 1: 4 rows) -- so X needs LDS only for X X^T, and
+// A and B are laid out in LDS with the same order of columns ("fragments":
+// 16 rows x 32 columns, 64 lanes x 8 values, hi then lo).  Blocks of 32 x 32 of
+// A on and below the diagonal belong to one wave each; where there are more
+// waves than blocks, groups of waves share out the columns of X X^T.
+// LDS reads bind it: a step reads 8 KB for each block and 32 columns of X, and
+// all of B for each strip.
+
+constexpr int FRAG = 2 * 512;  // values of a fragment
+constexpr int SMALL_W = 16;    // waves, at most
+
+struct SmallPlan {
+  int MT, NS;     // row tiles of 16 (even), strips of a wave
+  int W, NB, KS;  // waves, blocks, groups of waves for X X^T
+  int kp;         // columns, padded to 32
+  size_t lds;
+};
+
+// Four halves of a lane (rows r = 0..3 of its column) -> four columns of one
+// row: lanes 4q + t exchange so that lane t holds row t, columns 4q ..+3.
+__device__ __forceinline__ uint2 quad_turn(uint2 d, int t) {
+  const uint32_t sel = t & 1 ? 0x03020706u : 0x05040100u;
+  const uint32_t e0 = __builtin_amdgcn_mov_dpp((int)d.x, 0xB1, 0xF, 0xF, true);  // lane t ^ 1
+  const uint32_t e1 = __builtin_amdgcn_mov_dpp((int)d.y, 0xB1, 0xF, 0xF, true);
+  const uint32_t n0 = __builtin_amdgcn_perm(e0, d.x, sel), n1 = __builtin_amdgcn_perm(e1, d.y, sel);
+  const bool low = t < 2;
+  const uint32_t x = low ? n0 : n1, y = low ? n1 : n0;
+  const uint32_t z = __builtin_amdgcn_mov_dpp((int)y, 0x4E, 0xF, 0xF, true);  // lane t ^ 2
+  return low ? make_uint2(x, z) : make_uint2(z, x);
+}
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+// Four values split: [hi, lo], two dwords each.
+struct Split4 {
+  uint2 part[2];
+};
+__device__ __forceinline__ Split4 split4(f32x4 v) {
+  uint32_t h[2], l[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const f32x2 x = {v[2 * e], v[2 * e + 1]};
+    const f16x2 hi = __builtin_convertvector(x, f16x2);
+    const f32x2 rest = {fmaf(-LO_SCALE, (float)hi[0], LO_SCALE * x[0]), fmaf(-LO_SCALE, (float)hi[1], LO_SCALE * x[1])};
+    h[e] = __builtin_bit_cast(uint32_t, hi);
+    l[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, f16x2));
+  }
+  return {make_uint2(h[0], h[1]), make_uint2(l[0], l[1])};
+}
+
+// A lane's four values (rows of tile ti, a column of tile tj) -> fragments of
+// the matrix itself (rows ti, columns tj; steps of 32 columns) ..
+__device__ __forceinline__ void put_frag(_Float16* f, int ti, int tj, int steps, const Split4& v, int lane) {
+  const int t = lane & 3, c4 = (lane & 15) >> 2, g = lane >> 4;
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+    *reinterpret_cast<uint2*>(f + ((ti * steps + tj / 2) * 2 + part) * 512 + ((4 * g + t) + 16 * c4) * 8 + 4 * (tj & 1)) =
+        quad_turn(v.part[part], t);
+}
+// .. and of its transpose (rows tj, columns ti), where the lane's own values
+// lie side by side.
+__device__ __forceinline__ void put_frag_t(_Float16* f, int ti, int tj, int steps, const Split4& v, int lane) {
+#pragma unroll
+  for (int part = 0; part < 2; ++part)
+    *reinterpret_cast<uint2*>(f + ((tj * steps + ti / 2) * 2 + part) * 512 + lane * 8 + 4 * (ti & 1)) = v.part[part];
+}
+
+__device__ __forceinline__ void load_frag(const _Float16* f, int tile, int step, int steps, int lane, f16x8 (&d)[2]) {
+  const _Float16* q = f + (tile * steps + step) * FRAG + lane * 8;
+  d[0] = *reinterpret_cast<const f16x8*>(q);
+  d[1] = *reinterpret_cast<const f16x8*>(q + 512);
+}
+
+__device__ __forceinline__ void mfma3_16(const f16x8 (&a)[2], const f16x8 (&b)[2], f32x4& acc, f32x4& low) {
+  low = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[1], low, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[0], b[0], acc, 0, 0, 0);
+  low = __builtin_amdgcn_mfma_f32_16x16x32_f16(a[1], b[0], low, 0, 0, 0);
+}
+
+// The 32 x 32 block (bi, bj) of F F^T over the steps [lo, hi).
+__device__ __forceinline__ void block_product(const _Float16* f, int bi, int bj, int lo, int hi, int steps, int lane,
+                                              f32x4 (&out)[2][2]) {
+  f32x4 acc[2][2] = {}, low[2][2] = {};
+#pragma unroll 1  // (more steps in flight cost registers that the callers need)
+  for (int s = lo; s < hi; ++s) {
+    f16x8 a[2][2], b[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_frag(f, bi * 2 + h, s, steps, lane, a[h]);
+    if (bi != bj) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_frag(f, bj * 2 + h, s, steps, lane, b[h]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int part = 0; part < 2; ++part) b[h][part] = a[h][part];
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) mfma3_16(a[x], b[y], acc[x][y], low[x][y]);
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) out[x][y] = acc[x][y] + low[x][y] * (1.f / LO_SCALE);
+}
+
+template <int DT, int MT, int NS, int NT>
+__global__ __launch_bounds__(NT) void ns_small_kernel(const void* gp, void* outp, int rows, int cols, int n_steps,
+                                                        SmallPlan pl) {
+  extern __shared__ char s_raw[];
+  __shared__ double s_norm[SMALL_W];
+  using E = typename DType<DT>::T;
+  constexpr int MS = MT / 2;            // steps of 32 over the rows
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g4 = lane >> 4;
+  const bool flip = rows > cols;
+  const int m = flip ? cols : rows, k = flip ? rows : cols, strips = pl.kp / 16, ksteps = pl.kp / 32;
+  const E* g = static_cast<const E*>(gp) + (size_t)blockIdx.x * rows * cols;
+  E* out = static_cast<E*>(outp) + (size_t)blockIdx.x * rows * cols;
+  _Float16* fx = reinterpret_cast<_Float16*>(s_raw);           // X's fragments, and (when they are read) ..
+  _Float16* fa = fx;                                           // .. A's, ..
+  _Float16* fb = fx + MT * MS * FRAG;                          // .. B's, ..
+  float* part = reinterpret_cast<float*>(fb);                  // .. or partial blocks of A before B is there
+
+  // a lane's place in G: element (i, j) of X
+  auto at = [&](int i, int j) { return (uint32_t)(flip ? j * cols + i : i * cols + j); };
+  f32x4 x[NS][MT];
+  double sum = 0.;
+#pragma unroll
+  for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+    for (int it = 0; it < MT; ++it)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = it * 16 + 4 * g4 + r, j = (w * NS + ns) * 16 + c;
+        x[ns][it][r] = i < m && j < k ? DType<DT>::to_f32(g[at(i, j)]) : 0.f;
+      }
+#pragma unroll
+  for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+    for (int it = 0; it < MT; ++it)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += (double)x[ns][it][r] * (double)x[ns][it][r];
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  if (lane == 0) s_norm[w] = sum;
+  __syncthreads();
+  sum = s_norm[0];
+  for (int q = 1; q < pl.W; ++q) sum += s_norm[q];
+  const double inv = sum == 0. ? 0. : 1. / sqrt(sum);
+#pragma unroll
+  for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+    for (int it = 0; it < MT; ++it)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[ns][it][r] = (float)((double)x[ns][it][r] * inv);
+
+  // this wave's block of the lower triangle, and (KS > 1) its part of the sum
+  int bi, bj;
+  lower_tile(w % pl.NB, bi, bj);
+  const int group = w / pl.NB, per = (ksteps + pl.KS - 1) / pl.KS;  // (groups from KS on have nothing to do)
+  const int lo = group < pl.KS ? group * per : ksteps, hi = lo + per < ksteps ? lo + per : ksteps;
+  auto put_block = [&](_Float16* f, const f32x4 (&v)[2][2]) {
+#pragma unroll
+    for (int xy = 0; xy < 4; ++xy) {
+      const int ti = bi * 2 + (xy >> 1), tj = bj * 2 + (xy & 1);
+      const Split4 parts = split4(v[xy >> 1][xy & 1]);
+      put_frag_t(f, ti, tj, MS, parts, lane);
+      if (bi != bj) put_frag(f, ti, tj, MS, parts, lane);
+    }
+  };
+  u32x4 xo[NS][MS][2];  // X as an operand: tiles 2s and 2s + 1 make a step
+  auto operand = [&](int ns, int it, const Split4& parts) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      xo[ns][it / 2][q][it % 2 * 2] = parts.part[q].x;
+      xo[ns][it / 2][q][it % 2 * 2 + 1] = parts.part[q].y;
+    }
+  };
+  for (int step = 0; step < n_steps; ++step) {
+#pragma unroll
+    for (int ns = 0; ns < NS; ++ns)
+      if (w * NS + ns < strips)
+#pragma unroll
+        for (int it = 0; it < MT; ++it) {
+          const Split4 parts = split4(x[ns][it]);
+          put_frag(fx, it, w * NS + ns, ksteps, parts, lane);
+          operand(ns, it, parts);
+        }
+    __syncthreads();
+    // A = X X^T
+    f32x4 a[2][2];
+    block_product(fx, bi, bj, lo, hi, ksteps, lane, a);
+    __syncthreads();
+    if (pl.KS > 1) {
+      float* at = part + (group - 1) * pl.NB * 1024 + (w % pl.NB) * 1024 + lane * 4;
+      if (group > 0 && group < pl.KS)
+#pragma unroll
+        for (int xy = 0; xy < 4; ++xy) *reinterpret_cast<f32x4*>(at + xy * 256) = a[xy >> 1][xy & 1];
+      __syncthreads();
+      if (group == 0)
+        for (int h = 1; h < pl.KS; ++h)
+#pragma unroll
+          for (int xy = 0; xy < 4; ++xy)
+            a[xy >> 1][xy & 1] += *reinterpret_cast<const f32x4*>(at + h * pl.NB * 1024 + xy * 256);
+    }
+    if (group == 0) put_block(fa, a);
+    __syncthreads();
+    // B = b A + c A A (over the partial blocks, which have been read)
+    if (group == 0) {
+      f32x4 v[2][2];
+      block_product(fa, bi, bj, 0, MS, MS, lane, v);
+#pragma unroll
+      for (int xy = 0; xy < 4; ++xy) v[xy >> 1][xy & 1] = NS_C * v[xy >> 1][xy & 1] + NS_B * a[xy >> 1][xy & 1];
+      put_block(fb, v);
+    }
+    __syncthreads();
+    // X <- a X + B X, strip by strip
+    if (w * NS < strips) {
+#pragma unroll
+      for (int it = 0; it < MT; ++it) {
+        f32x4 acc[NS] = {}, low[NS] = {};
+#pragma unroll
+        for (int s = 0; s < MS; ++s) {
+          f16x8 b[2];
+          load_frag(fb, it, s, MS, lane, b);
+#pragma unroll
+          for (int ns = 0; ns < NS; ++ns) {
+            const f16x8 v[2] = {__builtin_bit_cast(f16x8, xo[ns][s][0]), __builtin_bit_cast(f16x8, xo[ns][s][1])};
+            mfma3_16(b, v, acc[ns], low[ns]);
+          }
+        }
+#pragma unroll
+        for (int ns = 0; ns < NS; ++ns) x[ns][it] = NS_A * x[ns][it] + (acc[ns] + low[ns] * (1.f / LO_SCALE));
+        __builtin_amdgcn_sched_barrier(0);  // (B's tiles one at a time: what is read ahead holds registers)
+      }
+    }
+    __syncthreads();
+  }
+  // (the lane's place is made anew: offsets and bounds kept from the loads above would hold registers all the way)
+  int lane_again = lane;
+  asm volatile("" : "+v"(lane_again));
+  const int c_out = lane_again & 15, g_out = lane_again >> 4;
+#pragma unroll
+  for (int ns = 0; ns < NS; ++ns)
+#pragma unroll
+    for (int it = 0; it < MT; ++it)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = it * 16 + 4 * g_out + r, j = (w * NS + ns) * 16 + c_out;
+        if (i < m && j < k) out[at(i, j)] = DType<DT>::from_f32(x[ns][it][r]);
+      }
+}
+
+// Whether (and how) a matrix of this size runs in one workgroup.  As many
+// waves as there are strips and blocks (up to 16): a wave's chain of LDS reads,
+// products and exchanges is what takes the time (128 x 192, a step: 12 waves
+// 21200, 6 waves of two strips 25400, 4 of three 32300 cycles).
+bool small_plan(const OrthoArgs& o, SmallPlan* p) {
+  const int m = o.rows < o.cols ? o.rows : o.cols, k = o.rows < o.cols ? o.cols : o.rows;
+  if (m > 128) return false;
+  const int MB = (m + 31) / 32;
+  p->MT = 2 * MB;
+  p->kp = round_up(k, 32);
+  const int strips = p->kp / 16;
+  p->NS = 1;
+  while (p->NS * SMALL_W < strips) p->NS *= 2;
+  if (p->NS * p->MT > 8) return false;  // X's registers
+  p->NB = MB * (MB + 1) / 2;
+  const int need = (strips + p->NS - 1) / p->NS;
+  p->W = need > p->NB ? need : p->NB;
+  if (p->W < 4) p->W = 4;
+  if (MB > 2 && p->W > 12) return false;  // (128 registers a wave are too few there)
+  p->KS = p->W / p->NB < p->kp / 32 ? p->W / p->NB : p->kp / 32;
+  const size_t x = (size_t)p->MT * (p->kp / 32) * FRAG * 2, a = (size_t)p->MT * MB * FRAG * 2;
+  const size_t b = a > (size_t)(p->KS - 1) * p->NB * 4096 ? a : (size_t)(p->KS - 1) * p->NB * 4096;
+  p->lds = x > a + b ? x : a + b;
+  return true;
+}
+
+template <int DT, int MT, int NS, int NT>
+hipError_t run_small(const OrthoArgs& o, const SmallPlan& p, const void* g, void* out, hipStream_t s) {
+  if (p.lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)ns_small_kernel<DT, MT, NS, NT>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
+    if (e != hipSuccess) return e;
+  }
+  ns_small_kernel<DT, MT, NS, NT><<<o.n, 64 * p.W, p.lds, s>>>(g, out, o.rows, o.cols, o.steps, p);
+  return hipGetLastError();
+}
+// The registers that so many waves leave to each.
+template <int DT, int MT, int NS>
+hipError_t pick_small(const OrthoArgs& o, const SmallPlan& p, const void* g, void* out, hipStream_t s) {
+  if (p.W <= 8) return run_small<DT, MT, NS, 512>(o, p, g, out, s);
+  if constexpr (MT <= 4)
+    if (p.W > 12) return run_small<DT, MT, NS, 1024>(o, p, g, out, s);
+  return run_small<DT, MT, NS, 768>(o, p, g, out, s);
+}
+template <int DT>
+hipError_t launch_small(const OrthoArgs& o, const SmallPlan& p, const void* g, void* out, hipStream_t s) {
+  switch (p.MT * 16 + p.NS) {
+    case 2 * 16 + 1: return pick_small<DT, 2, 1>(o, p, g, out, s);
+    case 2 * 16 + 2: return pick_small<DT, 2, 2>(o, p, g, out, s);
+    case 2 * 16 + 4: return pick_small<DT, 2, 4>(o, p, g, out, s);
+    case 4 * 16 + 1: return pick_small<DT, 4, 1>(o, p, g, out, s);
+    case 4 * 16 + 2: return pick_small<DT, 4, 2>(o, p, g, out, s);
+    case 6 * 16 + 1: return pick_small<DT, 6, 1>(o, p, g, out, s);
+    default: return pick_small<DT, 8, 1>(o, p, g, out, s);
+  }
+}
+
+// ---- many workgroups per matrix ----
 
 struct OrthoLayout {
   int m, k, mp, kp;
@@ -417,9 +750,15 @@ void run_ortho(const OrthoArgs& o, const OrthoLayout& L, NsArgs p, hipStream_t s
 
 }  // namespace
 
-size_t ortho_workspace_bytes(const OrthoArgs& p) { return ortho_layout(p).bytes; }
+size_t ortho_workspace_bytes(const OrthoArgs& p) {
+  SmallPlan sp;
+  return small_plan(p, &sp) ? 0 : ortho_layout(p).bytes;
+}
 
 hipError_t launch_ortho(const OrthoArgs& o, const void* g, void* out, void* workspace, hipStream_t s) {
+  SmallPlan sp;
+  if (small_plan(o, &sp))
+    return o.dt == DT_F32 ? launch_small<DT_F32>(o, sp, g, out, s) : launch_small<DT_BF16>(o, sp, g, out, s);
   const OrthoLayout L = ortho_layout(o);
   char* ws = static_cast<char*>(workspace);
   auto half = [&](size_t off) { return reinterpret_cast<_Float16*>(ws + off); };
