@@ -241,12 +241,27 @@ __device__ __forceinline__ void put_tile(const NsArgs& p, size_t mat, int i0, in
     using E = typename DType<DT>::T;
     E* out = static_cast<E*>(p.out) + mat * p.rows * p.cols;
     const bool flip = p.rows > p.cols;
-    for (int q = tid; q < TS * TS; q += nt) {
-      const int c = q & 31, r = q >> 5;
-      const int i = flip ? c : r, j = flip ? r : c;
-      if (i0 + i < p.m && j0 + j < p.k)
-        out[flip ? (size_t)(j0 + j) * p.cols + i0 + i : (size_t)(i0 + i) * p.cols + j0 + j] =
-            DType<DT>::from_f32(res[i * LDT + j]);
+    // four values of a row of G at a time (r: the tile's row, or column, that runs down G); one store where rows keep
+    // to its alignment
+    const bool whole = p.cols % 4 == 0 && (reinterpret_cast<uintptr_t>(p.out) & (4 * sizeof(E) - 1)) == 0;
+    const int r0 = flip ? j0 : i0, c0 = flip ? i0 : j0;
+    for (int q = tid; q < TS * TS / 4; q += nt) {
+      const int c = (q & 7) * 4, r = q >> 3;
+      if (r0 + r >= p.rows || c0 + c >= p.cols) continue;
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = flip ? res[(c + e) * LDT + r] : res[r * LDT + c + e];
+      E* o = out + (size_t)(r0 + r) * p.cols + c0 + c;
+      if (whole) {
+        if constexpr (DT == DT_F32)
+          *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+        else
+          *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c0 + c + e < p.cols) o[e] = DType<DT>::from_f32(v[e]);
+      }
     }
   }
 }
@@ -263,11 +278,11 @@ __device__ __forceinline__ void fetch2(const _Float16* p, f16x8 (&d)[2]) {
 
 // Few tiles and short sums, where what counts is how soon a product is done:
 // one 32 x 32 tile per workgroup, whose waves share out the steps of the sum
-// and add their partial tiles through LDS.
-constexpr int NS_W = 4;      // waves of a workgroup
+// and add their partial tiles through LDS; 8 waves where that leaves a CU no
+// more than two workgroups (1 x 512x658 99 us, with 4 waves 104), else 4.
 constexpr int NS_AHEAD = 4;  // steps whose operands are loaded ahead
 
-template <int MODE, int DT>
+template <int MODE, int DT, int NS_W>
 __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles) {
   __shared__ float s[NS_W][TS * LDT];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -279,8 +294,9 @@ __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles)
   const _Float16* Q = op.Q + (size_t)tj * op.steps * BLOCK + lane * 8;
   const int per = (op.steps + NS_W - 1) / NS_W, lo = w * per, hi = lo + per < op.steps ? lo + per : op.steps;
   const int i0 = ti * TS, j0 = tj * TS, i = tid >> 3, j = (tid & 7) * 4;
+  const bool ends = w < 4;  // 256 threads finish 4 values each
   Finish<MODE> fin;
-  fin.load(p, mat, i0, j0, i, j);  // (early: it arrives while the products run)
+  if (ends) fin.load(p, mat, i0, j0, i, j);  // (early: it arrives while the products run)
   f32x16 acc = {}, low = {};
   f16x8 a[NS_AHEAD][2], b[NS_AHEAD][2];
 #pragma unroll
@@ -302,36 +318,35 @@ __global__ __launch_bounds__(64 * NS_W) void ns_tile_kernel(NsArgs p, int tiles)
   }
   acc_to_lds(acc, low, s[w], lane);
   __syncthreads();
-  f32x4 v = *reinterpret_cast<const f32x4*>(&s[0][i * LDT + j]);
+  if (ends) {
+    f32x4 v = *reinterpret_cast<const f32x4*>(&s[0][i * LDT + j]);
 #pragma unroll
-  for (int q = 1; q < NS_W; ++q) v += *reinterpret_cast<const f32x4*>(&s[q][i * LDT + j]);
-  *reinterpret_cast<f32x4*>(&s[0][i * LDT + j]) = fin(p, mat, i0, j0, i, j, v);
+    for (int q = 1; q < NS_W; ++q) v += *reinterpret_cast<const f32x4*>(&s[q][i * LDT + j]);
+    *reinterpret_cast<f32x4*>(&s[0][i * LDT + j]) = fin(p, mat, i0, j0, i, j, v);
+  }
   __syncthreads();
   put_tile<MODE, DT>(p, mat, i0, j0, s[0], tid, 64 * NS_W);
 }
 
-// Many tiles: each wave takes 64 x 64 values by itself, 12 matrix instructions
-// for 8 KB of operands; the four waves of a workgroup form 128 x 128, so that
-// every operand block is read by two of them and the second read meets it in
-// the L1 cache.  Two-dimensional sizes are padded to 128.
-constexpr int WIDE = 128;
-constexpr int WIDE_AHEAD = 8;  // (steps are multiples of it)
+// More tiles: 64 x 64 values per workgroup, again with the sum shared out over
+// its waves (12 matrix instructions a step for 8 KB of operands), two
+// workgroups per CU, one of which works while the other starts or ends.
+constexpr int MID = 64;
+constexpr int MID_AHEAD = 3;
 
 template <int MODE, int DT>
-__global__ __launch_bounds__(256, 1) void ns_wide_kernel(NsArgs p, int tiles) {
-  __shared__ float s[4][TS * LDT];
+__global__ __launch_bounds__(256, 2) void ns_mid_kernel(NsArgs p, int tiles) {
+  __shared__ float s[4][4][TS * LDT];  // [wave][32 x 32 tile]
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile tile = next_tile<MODE>(tiles, p.kp / WIDE);
+  const Tile tile = next_tile<MODE>(tiles, p.kp / MID);
   const size_t mat = tile.mat;
-  // above the diagonal: wave 2 writes it (no barrier follows)
-  if ((MODE == NS_GRAM || MODE == NS_POLY) && tile.ti == tile.tj && w == 1) return;
-  const int ti = tile.ti * 4 + (w >> 1) * 2, tj = tile.tj * 4 + (w & 1) * 2;  // in tiles of 32
   const Operands<MODE> op(p, mat);
   const size_t row = (size_t)op.steps * BLOCK;
-  const _Float16* P = op.P + ti * row + lane * 8;
-  const _Float16* Q = op.Q + tj * row + lane * 8;
+  const _Float16* P = op.P + (size_t)tile.ti * 2 * row + lane * 8;
+  const _Float16* Q = op.Q + (size_t)tile.tj * 2 * row + lane * 8;
+  const int per = (op.steps + 3) / 4, lo = w * per, hi = lo + per < op.steps ? lo + per : op.steps;
   f32x16 acc[2][2] = {}, low[2][2] = {};
-  f16x8 a[WIDE_AHEAD][2][2], b[WIDE_AHEAD][2][2];
+  f16x8 a[MID_AHEAD][2][2], b[MID_AHEAD][2][2];
   auto fetch = [&](int q, int st) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -339,43 +354,162 @@ __global__ __launch_bounds__(256, 1) void ns_wide_kernel(NsArgs p, int tiles) {
       fetch2(Q + h * row + (size_t)st * BLOCK, b[q][h]);
     }
   };
+  auto product = [&](int q) {
 #pragma unroll
-  for (int q = 0; q < WIDE_AHEAD; ++q) fetch(q, q);
-  for (int st = 0; st < op.steps; st += WIDE_AHEAD) {
+    for (int part = 0; part < 3; ++part)  // lo hi, hi lo, hi hi: no instruction waits for the one before
 #pragma unroll
-    for (int q = 0; q < WIDE_AHEAD; ++q) {
+      for (int xy = 0; xy < 4; ++xy) {
+        const int x = xy >> 1, y = xy & 1;
+        f32x16& d = part < 2 ? low[x][y] : acc[x][y];
+        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[q][x][part == 0], b[q][y][part == 1], d, 0, 0, 0);
+      }
+  };
+  // (past its last step a wave loads the last one again: no branch around loads in flight)
+  const int end = hi - 1;
 #pragma unroll
-      for (int part = 0; part < 3; ++part)  // lo hi, hi lo, hi hi: no instruction waits for the one before
+  for (int q = 0; q < MID_AHEAD; ++q) fetch(q, lo + q < end ? lo + q : end);
+  int st = lo;
+  for (; st + MID_AHEAD <= hi; st += MID_AHEAD) {
 #pragma unroll
-        for (int xy = 0; xy < 4; ++xy) {
-          const int x = xy >> 1, y = xy & 1;
-          f32x16& d = part < 2 ? low[x][y] : acc[x][y];
-          d = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[q][x][part == 0], b[q][y][part == 1], d, 0, 0, 0);
-        }
-      if (st + WIDE_AHEAD < op.steps) fetch(q, st + WIDE_AHEAD + q);
+    for (int q = 0; q < MID_AHEAD; ++q) {
+      product(q);
+      fetch(q, st + MID_AHEAD + q < end ? st + MID_AHEAD + q : end);
     }
   }
+  if (st < hi) product(0);
+  if (st + 1 < hi) product(1);
+  const int x = w >> 1, y = w & 1, i0 = tile.ti * MID + x * TS, j0 = tile.tj * MID + y * TS;
+  Finish<MODE> fin[4];
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int u = 0; u < 4; ++u) fin[u].load(p, mat, i0, j0, (lane + u * 64) >> 3, (lane & 7) * 4);
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const int i0 = (ti + x) * TS, j0 = (tj + y) * TS;
-      if ((MODE == NS_GRAM || MODE == NS_POLY) && j0 > i0) continue;
-      Finish<MODE> fin[4];
+  for (int xy = 0; xy < 4; ++xy) acc_to_lds(acc[xy >> 1][xy & 1], low[xy >> 1][xy & 1], s[w][xy], lane);
+  __syncthreads();
+  if ((MODE == NS_GRAM || MODE == NS_POLY) && j0 > i0) return;  // (no barrier follows)
+  // each wave adds up and finishes one of the four
 #pragma unroll
-      for (int u = 0; u < 4; ++u) fin[u].load(p, mat, i0, j0, (lane + u * 64) >> 3, (lane & 7) * 4);
-      acc_to_lds(acc[x][y], low[x][y], s[w], lane);
-      wave_lds_sync();
+  for (int u = 0; u < 4; ++u) {
+    const int i = (lane + u * 64) >> 3, j = (lane & 7) * 4;
+    f32x4 v = *reinterpret_cast<const f32x4*>(&s[0][w][i * LDT + j]);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int i = (lane + u * 64) >> 3, j = (lane & 7) * 4;
-        f32x4* v = reinterpret_cast<f32x4*>(&s[w][i * LDT + j]);
-        *v = fin[u](p, mat, i0, j0, i, j, *v);
+    for (int q = 1; q < 4; ++q) v += *reinterpret_cast<const f32x4*>(&s[q][w][i * LDT + j]);
+    *reinterpret_cast<f32x4*>(&s[0][w][i * LDT + j]) = fin[u](p, mat, i0, j0, i, j, v);
+  }
+  wave_lds_sync();
+  put_tile<MODE, DT>(p, mat, i0, j0, s[0][w], lane, 64);
+}
+
+// Many tiles: a workgroup takes 128 x 128 values, each of its four waves
+// 64 x 64 of them.  Both operands go through LDS, where two waves read each
+// block; WIDE_STEPS steps are read while the next ones are written, whose
+// loads were issued WIDE_STEPS steps before.  What bounds it: a step takes 540
+// cycles, 384 of them matrix instructions, and on a full chip (4 x 1024x1024)
+// the clock falls from 2.3 to 1.6 GHz; start and end of a workgroup are 15000
+// of 50000 cycles there.  (Straight from the L1 cache a step takes 590 cycles:
+// 4 x 1024x1024 470 us instead of 460, 1 x 4096x4096 5060 instead of 4710.)
+constexpr int WIDE = 128;
+constexpr int WIDE_STEPS = 4;            // steps between barriers (sums have a multiple of 8)
+constexpr int WIDE_STEP = 16 * 512;      // values of a step: 4 row tiles of P, then of Q, hi and lo
+
+template <int MODE, int DT>
+__global__ __launch_bounds__(256, 1) void ns_wide_kernel(NsArgs p, int tiles) {
+  __shared__ _Float16 s_op[2][WIDE_STEPS][WIDE_STEP];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Tile tile = next_tile<MODE>(tiles, p.kp / WIDE);
+  const size_t mat = tile.mat;
+  const int ti = tile.ti * 4 + (w >> 1) * 2, tj = tile.tj * 4 + (w & 1) * 2;  // in tiles of 32
+  // above the diagonal: wave 2 writes it
+  const bool idle = (MODE == NS_GRAM || MODE == NS_POLY) && tile.ti == tile.tj && w == 1;
+  const Operands<MODE> op(p, mat);
+  const size_t row = (size_t)op.steps * BLOCK;
+  // this wave stages the hi or lo half of every second row tile
+  const _Float16* P = op.P + (size_t)(tile.ti * 4 + (w >> 1)) * row + (w & 1) * 512 + lane * 8;
+  const _Float16* Q = op.Q + (size_t)(tile.tj * 4 + (w >> 1)) * row + (w & 1) * 512 + lane * 8;
+  f16x8 in[WIDE_STEPS * 4];  // loads in flight: piece 4 q + i is block 4 i + w of step q
+  auto fetch = [&](int piece, int st) {
+    const int i = piece & 3;
+    const _Float16* src = (i < 2 ? P : Q) + (i & 1) * 2 * row;
+    in[piece] = *reinterpret_cast<const f16x8*>(src + (size_t)(st + piece / 4) * BLOCK);
+  };
+  auto put = [&](int buf, int piece) {
+    *reinterpret_cast<f16x8*>(&s_op[buf][piece / 4][((piece & 3) * 4 + w) * 512 + lane * 8]) = in[piece];
+  };
+  f32x16 acc[2][2] = {}, low[2][2] = {};
+  f16x8 o[2][8];  // operands of a step and of the next: P's two row tiles, then Q's, hi and lo
+  const int p0 = (w >> 1) * 4 * 512 + lane * 8, q0 = (8 + (w & 1) * 4) * 512 + lane * 8;
+  auto take = [&](int set, int buf, int q, int i) {
+    o[set][i] = *reinterpret_cast<const f16x8*>(&s_op[buf][q][(i < 4 ? p0 : q0) + (i & 3) * 512]);
+  };
+  auto product = [&](int set, int n) {  // lo hi, hi lo, hi hi: no instruction waits for the one before
+    const int part = n / 4, x = n >> 1 & 1, y = n & 1;
+    f32x16& d = part < 2 ? low[x][y] : acc[x][y];
+    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(o[set][x * 2 + (part == 0)], o[set][4 + y * 2 + (part == 1)], d, 0, 0, 0);
+  };
+  constexpr int PIECES = WIDE_STEPS * 4;
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) fetch(i, 0);
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    put(0, i);
+    fetch(i, WIDE_STEPS);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; ++i) take(0, 0, 0, i);
+  for (int st = 0; st < op.steps; st += 2 * WIDE_STEPS) {
+#pragma unroll
+    for (int buf = 0; buf < 2; ++buf) {
+      // (past the last step the first ones are loaded and written again: a branch here would make every write
+      // wait for all loads in flight)
+      const int at = st + buf * WIDE_STEPS, ahead = at + 2 * WIDE_STEPS < op.steps ? at + 2 * WIDE_STEPS : 0;
+      int done = 0;  // pieces written
+#pragma unroll
+      for (int q = 0; q < WIDE_STEPS; ++q) {
+        // One memory instruction after each matrix instruction, in this order: several in a row take longer to
+        // issue than the matrix instruction before them runs.  The other buffer is whole a step before it is read.
+        const bool last = q + 1 == WIDE_STEPS;
+        const int upto = last ? PIECES : (PIECES * (q + 1) + WIDE_STEPS - 2) / (WIDE_STEPS - 1);
+#pragma unroll
+        for (int n = 0; n < 12; ++n) {
+          product(q & 1, n);
+          __builtin_amdgcn_sched_barrier(0);
+          if (n < 8) {
+            take((q + 1) & 1, last ? buf ^ 1 : buf, last ? 0 : q + 1, n);
+            if (done < upto) put(buf ^ 1, done++);
+          } else {
+            fetch(q * 4 + n - 8, ahead);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (q + 2 == WIDE_STEPS) __syncthreads();
       }
-      wave_lds_sync();
-      put_tile<MODE, DT>(p, mat, i0, j0, s[w], lane, 64);
-      wave_lds_sync();
     }
+  }
+  __syncthreads();  // (the results go where the operands lie)
+  if (idle) return;  // (no barrier follows)
+  float* s = reinterpret_cast<float*>(s_op) + w * TS * LDT;
+  Finish<MODE> fin[4][4];
+#pragma unroll
+  for (int xy = 0; xy < 4; ++xy)  // (all at once: one wait; tiles above the diagonal are read and dropped)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      fin[xy][u].load(p, mat, (ti + (xy >> 1)) * TS, (tj + (xy & 1)) * TS, (lane + u * 64) >> 3, (lane & 7) * 4);
+#pragma unroll
+  for (int xy = 0; xy < 4; ++xy) {
+    const int i0 = (ti + (xy >> 1)) * TS, j0 = (tj + (xy & 1)) * TS;
+    if ((MODE == NS_GRAM || MODE == NS_POLY) && j0 > i0) continue;
+    acc_to_lds(acc[xy >> 1][xy & 1], low[xy >> 1][xy & 1], s, lane);
+    wave_lds_sync();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = (lane + u * 64) >> 3, j = (lane & 7) * 4;
+      f32x4* v = reinterpret_cast<f32x4*>(&s[i * LDT + j]);
+      *v = fin[xy][u](p, mat, i0, j0, i, j, *v);
+    }
+    wave_lds_sync();
+    put_tile<MODE, DT>(p, mat, i0, j0, s, lane, 64);
+    wave_lds_sync();
+  }
 }
 
 // ---- one workgroup per matrix ----
@@ -700,7 +834,7 @@ hipError_t launch_small(const OrthoArgs& o, const SmallPlan& p, const void* g, v
 
 struct OrthoLayout {
   int m, k, mp, kp;
-  bool wide;
+  int tile;
   size_t off_x, off_t0, off_t1, off_xf, off_a, off_b, bytes;
 };
 size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -708,8 +842,16 @@ OrthoLayout ortho_layout(const OrthoArgs& p) {
   OrthoLayout L;
   L.m = p.rows < p.cols ? p.rows : p.cols;
   L.k = p.rows < p.cols ? p.cols : p.rows;
-  L.wide = (int64_t)p.n * ((L.m + WIDE - 1) / WIDE) * ((L.k + WIDE - 1) / WIDE) >= 128;
-  const int pad = L.wide ? WIDE : TS;
+  // Larger tiles where there are enough of them (two workgroups of 64 x 64 to a CU, one of 128 x 128) and padding to
+  // them adds little.  Measured (us; 32 / 64 / 128): 12 x 512x512 255 / 237 / 287, 4 x 1024x1024 560 / 473 / 460,
+  // 1 x 4096x4096 - / 6460 / 4710, 64 x 130x140 (padded to 160, 192, 256) 112 / 165 / 240; with fewer tiles,
+  // 2 x 700x900 157 / 199 / -.
+  auto count = [&](int t) { return (int64_t)p.n * ((L.m + t - 1) / t) * ((L.k + t - 1) / t); };
+  auto work = [&](int t) { return (double)round_up(L.m, t) * round_up(L.m, t) * (3. * round_up(L.k, t) + round_up(L.m, t)); };
+  L.tile = TS;
+  if (count(MID) >= 512 && work(MID) <= 1.15 * work(TS)) L.tile = MID;
+  if (count(WIDE) >= 256 && work(WIDE) <= 1.15 * work(L.tile)) L.tile = WIDE;
+  const int pad = L.tile;
   L.mp = round_up(L.m, pad);
   L.kp = round_up(L.k, pad);
   const size_t x = (size_t)p.n * L.mp * L.kp * 4, a = (size_t)p.n * L.mp * L.mp * 4;  // 4 bytes a value, split or not
@@ -725,10 +867,12 @@ OrthoLayout ortho_layout(const OrthoArgs& p) {
 
 template <int MODE, int DT>
 void run_product(const OrthoArgs& o, const OrthoLayout& L, const NsArgs& p, hipStream_t s) {
-  const int t = L.wide ? WIDE : TS, mt = L.mp / t;
+  const int t = L.tile, mt = L.mp / t;
   const int tiles = MODE == NS_GRAM || MODE == NS_POLY ? mt * (mt + 1) / 2 : mt * (L.kp / t);
-  if (L.wide) ns_wide_kernel<MODE, DT><<<tiles * o.n, 256, 0, s>>>(p, tiles);
-  else ns_tile_kernel<MODE, DT><<<tiles * o.n, 64 * NS_W, 0, s>>>(p, tiles);
+  if (t == MID) ns_mid_kernel<MODE, DT><<<tiles * o.n, 256, 0, s>>>(p, tiles);
+  else if (t == WIDE) ns_wide_kernel<MODE, DT><<<tiles * o.n, 256, 0, s>>>(p, tiles);
+  else if (tiles * o.n <= 512) ns_tile_kernel<MODE, DT, 8><<<tiles * o.n, 512, 0, s>>>(p, tiles);
+  else ns_tile_kernel<MODE, DT, 4><<<tiles * o.n, 256, 0, s>>>(p, tiles);
 }
 
 template <int DT>

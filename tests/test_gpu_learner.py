@@ -495,6 +495,19 @@ def test_orthogonalize(size, dt):
         _check_ortho(g, R.orthogonalize(g))
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", [(12, 512, 448), (17, 512, 520), (17, 517, 512), (9, 500, 1001), (12, 449, 511)])
+def test_orthogonalize_stacks(size, dt):
+    """Stacks that take larger tiles, of three matrices over and over: equal ones come out equal to the bit."""
+    rng = np.random.default_rng(sum(size))
+    three = np.concatenate([_matrix(kind, 1, *size[1:], rng) for kind in ("normal", "lowrank", "decay")])
+    g = torch.from_numpy(three.astype(np.float32)).to(TDT[dt]).cuda()
+    out = R.orthogonalize(g.repeat(size[0] // 3 + 1, 1, 1)[:size[0]].contiguous())
+    _check_ortho(g, out[:3])
+    for i in range(3, size[0]):
+        assert torch.equal(out[i], out[i % 3]), i
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 8])
 def test_orthogonalize_steps(steps):
     rng = np.random.default_rng(steps)
