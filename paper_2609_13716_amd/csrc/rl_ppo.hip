@@ -1,16 +1,20 @@
 // Proximal policy optimisation's loss over stored rows and its gradients.
 //
-// A row's work is its softmax; what bounds it is HBM (8 bytes an action and 28
-// a row, both directions).  A wave takes 64 consecutive rows: their 64 nA
-// logits are read as nA coalesced dwords per lane and turned into one row per
-// lane through LDS (row stride odd, so that lanes hit different banks; illegal
-// actions become -inf on the way), and the gradients go back the same way.
+// A row's work is its softmax: 8 bytes an action and 28 a row against some 40
+// instructions an action and 250 a row, so that HBM and the vector units are
+// busy for about as long.  A wave takes 64 consecutive rows: their 64 nA logits
+// are read as 16 nA pieces of 16 bytes and turned into one row per lane through
+// LDS (illegal actions become -inf on the way), the row stays in registers, and
+// the gradients go back the same way.  1048576 rows of 6 take 29 us, 20 of them
+// for the rows (4.1 TB/s), the rest for the two other launches.
 // Sums over rows are float64, taken in an order that depends on the sizes only:
 // per lane, wave, workgroup, then over workgroups by the launch that follows.
 //   R <= PPO_SMALL   one workgroup does everything in one launch (500 rows of
 //                    6: 7 us of GPU time; 15 in three launches);
 //   otherwise        the advantages' sums (when they are normalised or rows
 //                    masked out), the rows, the six means.
+#include <utility>
+
 #include "rl_internal.h"
 
 namespace rl {
@@ -21,9 +25,9 @@ constexpr int PPO_SUM_NT = 1024;    // of one that adds up advantages
 constexpr int64_t PPO_SMALL = 2048;
 constexpr int PPO_ADV_B = 64, PPO_ROW_B = 512;  // workgroups, at most (their partial sums go to the workspace)
 constexpr int PPO_STATS = 6;
-constexpr int PPO_CHUNK = 8;        // dwords of a row tile that a lane has in flight
 
 struct PpoPart {  // workspace
+  double shift;              // what the advantages' sums are taken from
   double adv[PPO_ADV_B][3];  // rows counted, sum and sum of squares of their advantages
   double stat[PPO_ROW_B][PPO_STATS];
 };
@@ -76,12 +80,23 @@ __device__ __forceinline__ double stats_sum(const double (&v)[PPO_STATS], double
   return t;
 }
 
-__device__ __forceinline__ void adv_sums(const PpoArgs& p, int64_t first, int64_t step, double (&v)[3]) {
+// An advantage that the sums are taken from, so that a mean far from 0 costs
+// no digits of the variance: the first counted one of 64 rows spread evenly.
+__device__ __forceinline__ double adv_shift(const PpoArgs& p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = lane * p.R / 64;
+  const float a = p.adv[r];
+  const uint64_t some = __ballot((!p.mask || p.mask[r]) && fabsf(a) < INFINITY);
+  return some ? (double)__shfl(a, __ffsll((unsigned long long)some) - 1, 64) : 0.;
+}
+
+// Counted rows, and the sum and sum of squares of their advantages less `shift`.
+__device__ __forceinline__ void adv_sums(const PpoArgs& p, double shift, int64_t first, int64_t step, double (&v)[3]) {
 #pragma unroll 8
   for (int64_t r = first; r < p.R; r += step) {
     const uint8_t in = p.mask ? p.mask[r] : 1;
     const float read = p.adv[r];  // (before the mask is known; a padded row's value is dropped)
-    const double a = in ? (double)read : 0.;
+    const double a = in ? (double)read - shift : 0.;
     v[0] += in ? 1. : 0.;
     v[1] += a;
     v[2] += a * a;
@@ -92,11 +107,11 @@ struct PpoNorm {
   double inv_n, mean, rstd;
 };
 // From the counted rows' number, sum and sum of squares.
-__device__ __forceinline__ PpoNorm ppo_norm(const PpoArgs& p, const double (&v)[3]) {
+__device__ __forceinline__ PpoNorm ppo_norm(const PpoArgs& p, double shift, const double (&v)[3]) {
   PpoNorm r{1. / (v[0] > 0. ? v[0] : 1.), 0., 1.};
   if (p.normalize) {
-    const double var = v[2] * r.inv_n - v[1] * r.inv_n * (v[1] * r.inv_n);
-    r.mean = v[1] * r.inv_n;
+    const double off = v[1] * r.inv_n, var = v[2] * r.inv_n - off * off;
+    r.mean = shift + off;
     r.rstd = 1. / (sqrt(var < 0. ? 0. : var) + 1e-8);  // (a NaN stays one)
   }
   return r;
@@ -109,139 +124,159 @@ __device__ __forceinline__ double uniform(double v) {
   return __longlong_as_double((uint64_t)hi << 32 | lo);
 }
 
-// exp(x) for x <= 0: the hardware's 2^t with t = x log2(e) rounded, times
-// 1 + ln(2) (x log2(e) - t); within 3 float32 steps (results below 2^-126 are 0).
-__device__ __forceinline__ float exp_neg(float x) {
+// exp(x): the hardware's 2^t with t = x log2(e) rounded, times
+// 1 + ln(2) (x log2(e) - t); within 3 float32 steps for |x| < 2^100 (results
+// below 2^-126 are 0).
+__device__ __forceinline__ float exp32(float x) {
   constexpr float L2E = 1.4426950408889634f, L2E_LO = (float)(1.4426950408889634 - (double)L2E);
   const float t = x * L2E, r = fmaf(x, L2E_LO, fmaf(x, L2E, -t));
   return __builtin_amdgcn_exp2f(t) * fmaf(r, 0.6931471805599453f, 1.f);
 }
+// log(x) for x >= 1: the hardware's logarithm to base 2 times ln(2) in two parts.
+__device__ __forceinline__ float log32(float x) {
+  constexpr float LN2 = 0.6931471805599453f, LN2_LO = (float)(0.6931471805599453 - (double)LN2);
+  const float t = __builtin_amdgcn_logf(x);
+  return fmaf(t, LN2, t * LN2_LO);
+}
+// 1 / x for x >= 1: the hardware's, and one Newton step.
+__device__ __forceinline__ float rcp32(float x) {
+  const float r = __builtin_amdgcn_rcpf(x);
+  return fmaf(fmaf(-x, r, 1.f), r, r);
+}
 
 // exp(x) in float64, to 1e-13: 2^k times the Taylor sum of exp(r) to r^12 / 12!
-// for |r| <= ln(2) / 2 (the next term is below 2e-16).  Few registers: the
-// rows that need it are rare, and what it holds all of them pay for.
+// for |r| <= ln(2) / 2 (the next term is below 2e-16).  The rows that need it
+// are rare; its coefficients stay in memory so that the others do not hold
+// registers for them.
+__constant__ double INV_FACTORIAL[13] = {
+    1.,         1.,          1. / 2.,      1. / 6.,       1. / 24.,       1. / 120.,      1. / 720.,
+    1. / 5040., 1. / 40320., 1. / 362880., 1. / 3628800., 1. / 39916800., 1. / 479001600.};
 __device__ __forceinline__ double exp64(double x) {
   const double k = rint(x * 1.4426950408889634);
   const double r = fma(-k, 0.6931471805599453, x);
-  double s = 1. / 479001600.;
-  s = fma(s, r, 1. / 39916800.);
-  s = fma(s, r, 1. / 3628800.);
-  s = fma(s, r, 1. / 362880.);
-  s = fma(s, r, 1. / 40320.);
-  s = fma(s, r, 1. / 5040.);
-  s = fma(s, r, 1. / 720.);
-  s = fma(s, r, 1. / 120.);
-  s = fma(s, r, 1. / 24.);
-  s = fma(s, r, 1. / 6.);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.);
-  s = fma(s, r, 1.);
+  double s = 0.;
+#pragma unroll 1
+  for (int i = 12; i >= 0; --i) s = fma(s, r, INV_FACTORIAL[i]);
   return ldexp(s, (int)fmax(fmin(k, 2000.), -2000.));
 }
 
-// LDS floats of a row: odd, so that lanes of neighbouring rows hit different banks.
-__host__ __device__ inline int ppo_ld(int na) { return na | 1; }
+// LDS floats from a row to the next.  Values lie there as they lie in memory,
+// so that a lane moves four at a time without knowing their rows; rows of a
+// multiple of 8 (whose 64 starts would share few banks) are 4 floats apart.
+__host__ __device__ constexpr int ppo_ld(int na) { return na % 8 == 0 ? na + 4 : na; }
 
 // A logit less the row's largest; far below zero for an illegal action (so
 // that its probability is 0 and a product with it is, too).
-__device__ __forceinline__ float below_top(float x, float top) { return x == -INFINITY ? -1e30f : x - top; }
+constexpr float FAR_BELOW = -1e30f;
+__device__ __forceinline__ float below_top(float x, float top) { return x == -INFINITY ? FAR_BELOW : x - top; }
 
-// A wave's walk over the values of its 64 rows, 64 neighbouring ones at a
-// time: where value 64 j + lane lies in LDS, for j = 0, 1, ..
-struct Walk {
-  int at, col, na, skip, dq, dr;
-  __device__ Walk(int lane, int na) : na(na) {
-    const int ld = ppo_ld(na), row = lane / na;
-    dq = 64 / na * ld;
-    dr = 64 % na;
-    col = lane - row * na;
-    at = row * ld + col;
-    skip = ld - na;  // from the end of a row to the next
+// A lane's row in LDS -> registers, and back, by the widest pieces that every
+// row is aligned to.
+template <int NA>
+__device__ __forceinline__ void row_in(const float* x, float (&z)[NA]) {
+  constexpr int V = NA % 4 == 0 ? 4 : NA % 2 == 0 ? 2 : 1;
+  typedef float vec __attribute__((ext_vector_type(V)));
+#pragma unroll
+  for (int i = 0; i < NA; i += V) {
+    const vec v = *reinterpret_cast<const vec*>(x + i);
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[i + k] = v[k];
   }
-  __device__ void next() {
-    at += dq + dr;
-    col += dr;
-    if (col >= na) {
-      col -= na;
-      at += skip;
-    }
+}
+template <int NA>
+__device__ __forceinline__ void row_out(float* x, const float (&z)[NA]) {
+  constexpr int V = NA % 4 == 0 ? 4 : NA % 2 == 0 ? 2 : 1;
+  typedef float vec __attribute__((ext_vector_type(V)));
+#pragma unroll
+  for (int i = 0; i < NA; i += V) {
+    vec v;
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = z[i + k];
+    *reinterpret_cast<vec*>(x + i) = v;
   }
-};
+}
 
-// The 64 rows from r0 on, by one wave: gradients written, st added to.
+// The 64 rows from r0 on, by one wave: gradients written, st added to.  A
+// row's values stay in registers (the number of actions is a compile-time
+// constant for that).
+template <int NA>
 __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, int64_t r0, float* s,
                                          double (&st)[PPO_STATS]) {
-  const int lane = threadIdx.x & 63, na = p.NA;
-  const int live = p.R - r0 < 64 ? (int)(p.R - r0) : 64, vals = live * na;
-  const int64_t r = r0 + lane;
-  const bool counted = lane < live && (!p.mask || p.mask[r]);
-  int act = -1;
-  float old = 0.f, adv_in = 0.f, value = 0.f, value_old = 0.f, ret = 0.f;
-  if (counted) {
-    act = p.actions[r];
-    old = p.logp_old[r];
-    adv_in = p.adv[r];
-    value = p.value[r];
-    ret = p.ret[r];
-    if (p.value_clip > 0.f) value_old = p.value_old[r];
-  }
-  const float* x_in = p.logits + r0 * na;
-  const uint8_t* l_in = p.legal ? p.legal + r0 * na : nullptr;
-  Walk to(lane, na);
-  for (int j0 = 0; j0 < na; j0 += PPO_CHUNK) {
-    float in[PPO_CHUNK];
-    uint8_t ok[PPO_CHUNK];
+  constexpr int LD = ppo_ld(NA), Q = (NA + 3) / 4;  // (16 NA times four values)
+  const int lane = threadIdx.x & 63;
+  const int live = p.R - r0 < 64 ? (int)(p.R - r0) : 64, vals = live * NA;
+  const bool real = lane < live;
+  const uint32_t r = real ? lane : live - 1;  // (lanes past the last row read it again and count for nothing)
+  const bool counted = real && (!p.mask || (p.mask + r0)[r]);
+  const int act_in = (p.actions + r0)[r];
+  const float old = (p.logp_old + r0)[r], adv_in = (p.adv + r0)[r], value = (p.value + r0)[r], ret = (p.ret + r0)[r];
+  const float value_old = p.value_clip > 0.f ? (p.value_old + r0)[r] : 0.f;
+  const float* x_in = p.logits + r0 * NA;
+  const uint8_t* l_in = p.legal ? p.legal + r0 * NA : nullptr;
+  auto at = [](int v) { return LD == NA ? v : v + (LD - NA) * (v / NA); };  // value v of the 64 rows in LDS
+  if (live == 64 && ((reinterpret_cast<uintptr_t>(p.logits) & 15) | (reinterpret_cast<uintptr_t>(p.legal) & 3)) == 0) {
+    f32x4 in[Q];
+    uint32_t ok[Q];
 #pragma unroll
-    for (int j = 0; j < PPO_CHUNK; ++j) {
-      const int e = (j0 + j) * 64 + lane;
-      in[j] = -INFINITY;
-      ok[j] = 1;
-      if (e < vals) {
-        in[j] = x_in[e];
-        if (l_in) ok[j] = l_in[e];
+    for (int q = 0; q < Q; ++q) {
+      const int v = (q * 64 + lane) * 4;
+      if ((q + 1) * 256 <= 64 * NA || v < 64 * NA) {
+        in[q] = *reinterpret_cast<const f32x4*>(x_in + v);
+        if (l_in) ok[q] = *reinterpret_cast<const uint32_t*>(l_in + v);
       }
     }
 #pragma unroll
-    for (int j = 0; j < PPO_CHUNK; ++j)
-      if (j0 + j < na) {  // (rows past the last one: -inf)
-        s[to.at] = ok[j] ? in[j] : -INFINITY;
-        to.next();
-      }
+    for (int q = 0; q < Q; ++q) {
+      const int v = (q * 64 + lane) * 4;
+      if (l_in)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) in[q][k] = ok[q] >> 8 * k & 255 ? in[q][k] : -INFINITY;
+      if ((q + 1) * 256 <= 64 * NA || v < 64 * NA) *reinterpret_cast<f32x4*>(s + at(v)) = in[q];
+    }
+  } else {  // (rows past the last one hold what was there: they count for nothing)
+#pragma unroll 4
+    for (int v = lane; v < vals; v += 64) {
+      const float in = x_in[v];
+      s[at(v)] = !l_in || l_in[v] ? in : -INFINITY;
+    }
   }
+  const int act = counted ? act_in : -1;
   wave_lds_sync();
-  float* x = s + lane * ppo_ld(na);
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int i = 0; i < na; ++i) top = x[i] > top ? x[i] : top;  // (a NaN is met in the sum)
+  float* x = s + lane * LD;
+  float z[NA], e[NA], top = -INFINITY;
+  row_in<NA>(x, z);
+#pragma unroll
+  for (int i = 0; i < NA; ++i) top = z[i] > top ? z[i] : top;  // (a NaN is met in the sum)
+  const float xa = act >= 0 && act < NA ? x[act] : -INFINITY;
   float sum = 0.f, zsum = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < na; ++i) {
-    const float z = below_top(x[i], top), e = exp_neg(z);
-    sum += e;
-    zsum += e * z;
+#pragma unroll
+  for (int i = 0; i < NA; ++i) {
+    z[i] = below_top(z[i], top);
+    e[i] = exp32(z[i]);
+    sum += e[i];
+    zsum = fmaf(e[i], z[i], zsum);
   }
   const bool some = !(sum == 0.f);  // a legal action's term is 1, or NaN
-  const float logs = some ? logf(sum) : 0.f, inv = some ? 1.f / sum : 0.f;
+  const float logs = some ? log32(sum) : 0.f, inv = some ? rcp32(sum) : 0.f;
   const float ent = logs - zsum * inv;  // -sum p log p, log p = z - logs
   float slope = 0.f;                    // d policy / d log p_a
-  const float xa = act >= 0 && act < na ? x[act] : -INFINITY;
   if (!(xa == -INFINITY)) {
     const float adv = (float)(((double)adv_in - nm.mean) * nm.rstd);
-    const double lo = 1. - (double)p.clip, hi = 1. + (double)p.clip;
-    const float diff = xa - top - logs - old, ratio = expf(diff);
-    bool below = (double)ratio < lo, above = (double)ratio > hi;
-    // near a border the float32 ratio does not say on which side it lies
+    const float lo = (float)(1. - (double)p.clip), hi = (float)(1. + (double)p.clip);
+    const float diff = xa - top - logs - old, ratio = exp32(diff > 200.f ? 200.f : diff < -200.f ? -200.f : diff);
+    bool below = ratio < lo, above = ratio > hi;
+    // near a border the float32 ratio does not say on which side it lies (the borders' own rounding is within tol)
     const float tol = 1e-6f * (16.f + fabsf(xa) + fabsf(top) + fabsf(old)) * ratio;
-    if (fabs((double)ratio - lo) <= tol || fabs((double)ratio - hi) <= tol) {
+    if (fabsf(ratio - lo) <= tol || fabsf(ratio - hi) <= tol) {
       // (xa less the log of the sum, less old) against log(1 -+ clip), without logarithms
       double s64 = 0.;
 #pragma unroll 1
-      for (int i = 0; i < na; ++i) s64 += x[i] == -INFINITY ? 0. : exp64((double)x[i] - (double)top);
+      for (int i = 0; i < NA; ++i) s64 += x[i] == -INFINITY ? 0. : exp64((double)x[i] - (double)top);
       const double e64 = exp64((double)xa - (double)top - (double)old);
-      below = e64 < lo * s64;
-      above = e64 > hi * s64;
+      below = e64 < (1. - (double)p.clip) * s64;
+      above = e64 > (1. + (double)p.clip) * s64;
     }
-    const float clipped = above ? (float)hi : below ? (float)lo : ratio;
+    const float clipped = above ? hi : below ? lo : ratio;
     // the smaller surrogate is the plain one unless the ratio has left the range on the advantage's side
     const bool plain = adv > 0.f ? !above : adv < 0.f ? !below : true;
     st[1] -= (double)((plain ? ratio : clipped) * adv);
@@ -250,38 +285,42 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     st[5] += below || above ? 1. : 0.;
   }
   if (counted && some) st[3] += (double)ent;
-  if (lane < live) {
-    double dv = 0.;
-    if (counted) {
-      const double err = (double)value - ret, off = (double)value - value_old, vc = p.value_clip;
-      double loss = 0.5 * err * err;
-      dv = err;
-      if (vc > 0. && fabs(off) > vc) {
-        const double ec = value_old + (off > 0. ? vc : -vc) - ret;
-        if (0.5 * ec * ec > loss) {
-          loss = 0.5 * ec * ec;
-          dv = 0.;
-        }
+  double dv = 0.;
+  if (counted) {
+    const double err = (double)value - ret, off = (double)value - value_old, vc = p.value_clip;
+    double loss = 0.5 * err * err;
+    dv = err;
+    if (vc > 0. && fabs(off) > vc) {
+      const double ec = value_old + (off > 0. ? vc : -vc) - ret;
+      if (0.5 * ec * ec > loss) {
+        loss = 0.5 * ec * ec;
+        dv = 0.;
       }
-      st[2] += loss;
     }
-    p.dvalue[r] = (float)((double)p.value_coef * dv * nm.inv_n);
+    st[2] += loss;
   }
-  const float inv_n = (float)nm.inv_n, c = p.entropy_coef, shift = ent - logs;
+  if (real) (p.dvalue + r0)[r] = (float)((double)p.value_coef * dv * nm.inv_n);
+  // slope (onehot - p) + c p (log p + H), over n
+  const float inv_n = (float)nm.inv_n, c = p.entropy_coef, shift = ent - logs, back = slope * inv_n;
   const bool any = counted && some;
-#pragma unroll 4
-  for (int i = 0; i < na; ++i) {
-    const float z = below_top(x[i], top), pi = exp_neg(z) * inv;
-    const float d = (slope * ((i == act ? 1.f : 0.f) - pi) + c * pi * (z + shift)) * inv_n;
-    x[i] = any && !(x[i] == -INFINITY) ? d : 0.f;
+#pragma unroll
+  for (int i = 0; i < NA; ++i) {
+    const float d = fmaf(e[i] * inv, (c * (z[i] + shift) - slope) * inv_n, i == act ? back : 0.f);
+    z[i] = any && !(z[i] == FAR_BELOW) ? d : 0.f;
   }
+  row_out<NA>(x, z);
   wave_lds_sync();
-  Walk from(lane, na);
+  float* out = p.dlogits + r0 * NA;
+  if (live == 64 && (reinterpret_cast<uintptr_t>(p.dlogits) & 15) == 0) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int v = (q * 64 + lane) * 4;
+      if ((q + 1) * 256 <= 64 * NA || v < 64 * NA)
+        *reinterpret_cast<f32x4*>(out + v) = *reinterpret_cast<const f32x4*>(s + at(v));
+    }
+  } else {
 #pragma unroll 4
-  for (int j = 0; j < na; ++j) {
-    const int e = j * 64 + lane;
-    if (e < vals) p.dlogits[r0 * na + e] = s[from.at];
-    from.next();
+    for (int v = lane; v < vals; v += 64) out[v] = s[at(v)];
   }
   wave_lds_sync();  // (the next rows overwrite s)
 }
@@ -295,19 +334,26 @@ __device__ __forceinline__ void ppo_means(const PpoArgs& p, const double (&v)[PP
 __global__ __launch_bounds__(PPO_SUM_NT) void ppo_adv_kernel(PpoArgs p, PpoPart* part) {
   __shared__ double s[16][3];
   double v[3] = {0., 0., 0.};
-  adv_sums(p, (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, (int64_t)gridDim.x * PPO_SUM_NT, v);
+  const double shift = p.normalize ? adv_shift(p) : 0.;
+  if (blockIdx.x == 0 && threadIdx.x == 0) part->shift = shift;
+  adv_sums(p, shift, (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, (int64_t)gridDim.x * PPO_SUM_NT, v);
   block_sum<3>(v, s);
   if (threadIdx.x == 0)
     for (int i = 0; i < 3; ++i) part->adv[blockIdx.x][i] = v[i];
 }
 
 // LDS bytes of a wave: its rows, or its statistics at the end.
-__host__ __device__ inline int ppo_wave_bytes(int na) {
+__host__ __device__ constexpr int ppo_wave_bytes(int na) {
   const int rows = 4 * 64 * ppo_ld(na);
   return rows > TURN_BYTES ? rows : TURN_BYTES;
 }
 
-__global__ __launch_bounds__(PPO_NT) void ppo_rows_kernel(PpoArgs p, PpoPart* part, int adv_blocks) {
+// Up to 20 actions the registers are held to what four waves of a SIMD may
+// have (two workgroups to a CU; at 20 that spills 8 dwords: 655361 masked rows
+// 45 us, 51 without); beyond, too much would be spilled (400000 rows of 24: 52
+// us, 42 without).
+template <int NA>
+__global__ __launch_bounds__(PPO_NT, NA <= 20 ? 4 : 1) void ppo_rows_kernel(PpoArgs p, PpoPart* part, int adv_blocks) {
   extern __shared__ double s_dyn[];
   __shared__ double s_stat[16][PPO_STATS];
   PpoNorm nm{1. / (double)p.R, 0., 1.};
@@ -317,13 +363,14 @@ __global__ __launch_bounds__(PPO_NT) void ppo_rows_kernel(PpoArgs p, PpoPart* pa
     if (b < adv_blocks)
       for (int i = 0; i < 3; ++i) v[i] = part->adv[b][i];
     wave_sum<3>(v);
-    nm = ppo_norm(p, v);
+    nm = ppo_norm(p, part->shift, v);
     nm = {uniform(nm.inv_n), uniform(nm.mean), uniform(nm.rstd)};
   }
   double st[PPO_STATS] = {0., 0., 0., 0., 0., 0.};
-  char* mine = reinterpret_cast<char*>(s_dyn) + (threadIdx.x >> 6) * ppo_wave_bytes(p.NA);
-  for (int64_t r0 = (int64_t)blockIdx.x * PPO_NT + (threadIdx.x & ~63); r0 < p.R; r0 += (int64_t)gridDim.x * PPO_NT)
-    ppo_rows(p, nm, r0, reinterpret_cast<float*>(mine), st);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), step = blockDim.x;
+  char* mine = reinterpret_cast<char*>(s_dyn) + w * ppo_wave_bytes(NA);
+  for (int64_t r0 = (int64_t)blockIdx.x * step + w * 64; r0 < p.R; r0 += (int64_t)gridDim.x * step)
+    ppo_rows<NA>(p, nm, r0, reinterpret_cast<float*>(mine), st);
   const double t = stats_sum(st, reinterpret_cast<double*>(mine), s_stat);
   if (threadIdx.x < PPO_STATS) part->stat[blockIdx.x][threadIdx.x] = t;
 }
@@ -352,17 +399,20 @@ __global__ __launch_bounds__(STATS_NT) void ppo_stats_kernel(PpoArgs p, const Pp
 }
 
 // Everything in one workgroup.
-__global__ __launch_bounds__(1024) void ppo_small_kernel(PpoArgs p) {
+template <int NA>
+__global__ __launch_bounds__(PPO_NT) void ppo_small_kernel(PpoArgs p) {
   extern __shared__ double s_dyn[];
   __shared__ double s_adv[16][3], s_stat[16][PPO_STATS], s_all[PPO_STATS];
   double v[3] = {0., 0., 0.};
-  adv_sums(p, threadIdx.x, blockDim.x, v);
+  const double shift = p.normalize ? adv_shift(p) : 0.;
+  adv_sums(p, shift, threadIdx.x, blockDim.x, v);
   block_sum<3>(v, s_adv);
-  const PpoNorm nm = ppo_norm(p, v);
+  const PpoNorm nm = ppo_norm(p, shift, v);
   double st[PPO_STATS] = {0., 0., 0., 0., 0., 0.};
-  char* mine = reinterpret_cast<char*>(s_dyn) + (threadIdx.x >> 6) * ppo_wave_bytes(p.NA);
-  for (int64_t r0 = threadIdx.x & ~63; r0 < p.R; r0 += blockDim.x)
-    ppo_rows(p, nm, r0, reinterpret_cast<float*>(mine), st);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  char* mine = reinterpret_cast<char*>(s_dyn) + w * ppo_wave_bytes(NA);
+  for (int64_t r0 = w * 64; r0 < p.R; r0 += blockDim.x)
+    ppo_rows<NA>(p, nm, r0, reinterpret_cast<float*>(mine), st);
   const double t = stats_sum(st, reinterpret_cast<double*>(mine), s_stat);
   if (threadIdx.x < PPO_STATS) s_all[threadIdx.x] = t;
   wave_lds_sync();
@@ -370,27 +420,39 @@ __global__ __launch_bounds__(1024) void ppo_small_kernel(PpoArgs p) {
   ppo_means(p, st, nm.inv_n);
 }
 
+template <int NA>
+hipError_t run_ppo(const PpoArgs& p, void* workspace, hipStream_t s) {
+  const size_t wave = ppo_wave_bytes(NA);
+  if (p.R <= PPO_SMALL) {
+    const int most = (int)((60u << 10) / wave), rows = (int)((p.R + 63) / 64);  // waves that fit in LDS; row tiles
+    const int waves = rows < most ? rows : most;
+    const int n = waves < PPO_NT / 64 ? waves : PPO_NT / 64;
+    ppo_small_kernel<NA><<<1, 64 * n, wave * n, s>>>(p);
+    return hipGetLastError();
+  }
+  PpoPart* part = static_cast<PpoPart*>(workspace);
+  const int nt = wave * (PPO_NT / 64) > 62 * 1024 ? PPO_NT / 2 : PPO_NT;  // (a workgroup has 64 KB of LDS)
+  const int64_t tiles = (p.R + nt - 1) / nt, sums = (p.R + PPO_SUM_NT - 1) / PPO_SUM_NT;
+  const int blocks = (int)(tiles < PPO_ROW_B ? tiles : PPO_ROW_B);
+  const int adv_blocks = p.normalize || p.mask ? (int)(sums < PPO_ADV_B ? sums : PPO_ADV_B) : 0;
+  if (adv_blocks) ppo_adv_kernel<<<adv_blocks, PPO_SUM_NT, 0, s>>>(p, part);
+  ppo_rows_kernel<NA><<<blocks, nt, wave * (nt / 64), s>>>(p, part, adv_blocks);
+  ppo_stats_kernel<<<1, STATS_NT, 0, s>>>(p, part, adv_blocks, blocks);
+  return hipGetLastError();
+}
+
+template <int... N>
+hipError_t pick_ppo(std::integer_sequence<int, N...>, const PpoArgs& p, void* workspace, hipStream_t s) {
+  static constexpr hipError_t (*run[])(const PpoArgs&, void*, hipStream_t) = {run_ppo<N + 1>...};
+  return run[p.NA - 1](p, workspace, s);
+}
+
 }  // namespace
 
 size_t ppo_workspace_bytes(int64_t R) { return R <= PPO_SMALL ? 0 : sizeof(PpoPart); }
 
 hipError_t launch_ppo(const PpoArgs& p, void* workspace, hipStream_t s) {
-  const size_t wave = ppo_wave_bytes(p.NA);
-  if (p.R <= PPO_SMALL) {
-    const int most = (int)((60u << 10) / wave), rows = (int)((p.R + 63) / 64);  // waves that fit in LDS; row tiles
-    const int waves = rows < most ? rows : most;
-    const int n = waves < 16 ? waves : 16;
-    ppo_small_kernel<<<1, 64 * n, wave * n, s>>>(p);
-    return hipGetLastError();
-  }
-  PpoPart* part = static_cast<PpoPart*>(workspace);
-  const int64_t tiles = (p.R + PPO_NT - 1) / PPO_NT, sums = (p.R + PPO_SUM_NT - 1) / PPO_SUM_NT;
-  const int blocks = (int)(tiles < PPO_ROW_B ? tiles : PPO_ROW_B);
-  const int adv_blocks = p.normalize || p.mask ? (int)(sums < PPO_ADV_B ? sums : PPO_ADV_B) : 0;
-  if (adv_blocks) ppo_adv_kernel<<<adv_blocks, PPO_SUM_NT, 0, s>>>(p, part);
-  ppo_rows_kernel<<<blocks, PPO_NT, wave * (PPO_NT / 64), s>>>(p, part, adv_blocks);
-  ppo_stats_kernel<<<1, STATS_NT, 0, s>>>(p, part, adv_blocks, blocks);
-  return hipGetLastError();
+  return pick_ppo(std::make_integer_sequence<int, MAX_NA>(), p, workspace, s);
 }
 
 }  // namespace rl

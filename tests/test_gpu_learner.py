@@ -441,6 +441,29 @@ def test_ppo_borders():
         _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER), False)
 
 
+@pytest.mark.parametrize("rows", [900, 30000])
+@pytest.mark.parametrize("mean,scale", [(3000.0, 0.01), (-2e6, 1.0), (7.0, 0.0)])
+def test_ppo_advantages_far_from_zero(rows, mean, scale):
+    """A mean that is large against the spread, behind padding, too; and equal advantages, which normalise to 0."""
+    for padded in (False, True):
+        kw = _ppo(rows, 6, seed=12)
+        kw["adv"] = (mean + scale * np.random.default_rng(13).standard_normal(rows)).astype(np.float32)
+        if padded:
+            kw["mask"] = (np.arange(rows) >= rows * 3 // 4).astype(np.uint8)
+            kw["adv"][kw["mask"] == 0] = np.nan
+        got = R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True)
+        if scale == 0.0:
+            assert got[2][1] == 0 and bool(torch.isfinite(got[0]).all())
+        _check_ppo(kw, got, True)
+
+
+@pytest.mark.parametrize("nA", range(1, 33))
+def test_ppo_every_number_of_actions(nA):
+    for rows, off in ((193, 0), (2400, 0), (2115, 1)):
+        kw = _ppo(rows, nA, seed=nA, masked=True)
+        _check_ppo(kw, R.ppo_loss(**_gpu_args(kw, off=off), **HYPER), False)
+
+
 def test_ppo_nan_stays_in_its_row():
     kw = _ppo(500, 6, seed=7)
     clean = R.ppo_loss(**_gpu_args(kw), **HYPER)
