@@ -16,7 +16,9 @@
 //     through LDS and replay their steps from the state that reaches them
 //     (inputs stay in registers, so they are read once); and with very few
 //     channels the trajectory is cut into segments, one workgroup each, whose
-//     maps a first launch writes to the workspace (inputs are read twice).
+//     waves (which then take steps in a row, and never wait for one another)
+//     are folded to maps in the workspace by a first launch and replayed by a
+//     second (inputs are read twice).
 // Episode ends cut the state: a map that contains one does not read its input.
 // It is marked by SCAN_CUT in place of A, so that 0 * NaN never arises.
 #include <initializer_list>
@@ -229,7 +231,9 @@ __device__ __forceinline__ void states_read() {
 }
 
 // Workspace of a run cut into segments: slot 0 holds the constant map to the
-// state that enters the first segment, slot g + 1 the map of segment g.
+// state that enters the first segment, slot g + 1 the map of segment g; behind
+// the slots of all `segments` lie the maps of their waves, S to a segment (a
+// wave has seg / S steps in a row, so that no wave waits for another inside).
 template <bool DIAG>
 __device__ __forceinline__ Map<DIAG>* slot(void* ws, size_t N, int g) { return static_cast<Map<DIAG>*>(ws) + N * g; }
 
@@ -250,6 +254,45 @@ __device__ __forceinline__ void enter_segment(void* ws, size_t N, int g, int w, 
   for (int v = 0; v < V; ++v) carry[v] = Val<DIAG>::zero();
   ex(0, w, lane, mine, carry, into);
 }
+
+template <bool DIAG, int S>
+__device__ __forceinline__ Map<DIAG>* wave_slot(void* ws, size_t N, int segments, int g, int w) {
+  return slot<DIAG>(ws, N, segments + 1 + g * S + w);
+}
+
+// The state that enters wave w's part of segment g.
+template <bool DIAG, int V, int S>
+__device__ __forceinline__ void enter_part(void* ws, size_t N, int segments, int g, int w, int lane,
+                                           const Lane<DIAG, V>& l, Exchange<DIAG, V, S>& ex, Val<DIAG> (&carry)[V]) {
+  enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
+  for (int j = 0; j < w; ++j)
+#pragma unroll
+    for (int v = 0; v < V; ++v) carry[v] = wave_slot<DIAG, S>(ws, N, segments, g, j)[l.c + v](carry[v]);
+}
+
+// After a wave folded its part to `mine`: its map and the segment's.
+template <bool DIAG, int V, int S>
+__device__ __forceinline__ void leave_part(void* ws, size_t N, int segments, int g, int w, int lane,
+                                           const Lane<DIAG, V>& l, Exchange<DIAG, V, S>& ex,
+                                           const Map<DIAG> (&mine)[V]) {
+  ex.share(0, w, lane, mine);
+  if (!l.live) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    wave_slot<DIAG, S>(ws, N, segments, g, w)[l.c + v] = mine[v];
+    if (w == 0) {
+      Map<DIAG> all = mine[v];
+#pragma unroll
+      for (int j = 1; j < S; ++j) all = ex.m[0][j][v][lane].after(all);
+      slot<DIAG>(ws, N, g + 1)[l.c + v] = all;
+    }
+  }
+}
+
+// What a launch does: the whole run; or, where it is cut into segments, first
+// every wave's part folded to a map, then the parts replayed from the states
+// that enter them.
+enum { SCAN_WHOLE = 0, SCAN_FOLD = 1, SCAN_PARTS = 2 };
 
 // Inputs of SCAN_K steps of a wave, [first, end) of them real.
 template <int DT, bool DIAG, int V>
@@ -280,9 +323,8 @@ __device__ __forceinline__ void load_lambda(const void* gate, const Lane<DIAG, V
   }
 }
 
-// Forward.  AGG: fold this segment's steps into its workspace slot; otherwise
-// write h (and, in the last segment, h_last).  seg: steps of a segment.
-template <int DT, bool DIAG, int V, int S, bool AGG>
+// Forward.  seg: steps of a segment.
+template <int DT, bool DIAG, int V, int S, int MODE>
 __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u, const void* gate,
                                                       const uint8_t* done, const float* h0, void* h, float* h_last,
                                                       void* ws, int seg) {
@@ -292,61 +334,65 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u,
   const size_t N = (size_t)a.E * a.A * a.W;
   const Lane<DIAG, V> l(a, lane, scan_block<S>(N * (DIAG ? 2 : 1) * elem_bytes<DT>()));
   const int g = blockIdx.y;
-  const int first = g * seg, end = a.T - first < seg ? a.T : first + seg;
+  constexpr bool PARTS = MODE != SCAN_WHOLE;  // this wave's steps lie in a row
+  const int first = PARTS ? g * seg + w * (seg / S) : 0;
+  const int end = PARTS && a.T - first > seg / S ? first + seg / S : a.T;
+  constexpr int STEP = PARTS ? SCAN_K : S * SCAN_K;
   VT lam[V], carry[V], into[V];
   load_lambda<DT, DIAG, V>(gate, l, a.W, lam);
-  int buf = 0;
-  if (AGG || !ws) {
+  if constexpr (MODE == SCAN_PARTS) {
+    enter_part<DIAG, V, S>(ws, N, gridDim.y, g, w, lane, l, ex, carry);
+  } else {
     load_state<DIAG, V>(h0, l, a.W, carry);
-    if (AGG && g == 0 && w == 0 && l.live)
+    if (MODE == SCAN_FOLD && g == 0 && w == 0 && l.live)
 #pragma unroll
       for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
-  } else {
-    enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
-    buf = 1;
   }
-  Map<DIAG> all[V];  // AGG: everything so far
+  VT A[V], B[V];  // the steps so far (SCAN_FOLD) or of this block
+  bool cut = false;
+  auto restart = [&]() {
 #pragma unroll
-  for (int v = 0; v < V; ++v) all[v] = {VT::one(), VT::zero()};
-
+    for (int v = 0; v < V; ++v) {
+      A[v] = VT::one();
+      B[v] = VT::zero();
+    }
+    cut = false;
+  };
+  restart();
+  int buf = 0;
   Block<DT, DIAG, V> cur, nxt;
-  cur.load(a, l, u, gate, done, first + w * SCAN_K, end);
-  for (int t0 = first; t0 < end; t0 += S * SCAN_K) {
-    const int tw = t0 + w * SCAN_K;
-    if (t0 + S * SCAN_K < end) nxt.load(a, l, u, gate, done, tw + S * SCAN_K, end);
-    if constexpr (S > 1) {
-      Map<DIAG> mine[V];
+  const int ahead = PARTS ? 0 : w * SCAN_K;
+  cur.load(a, l, u, gate, done, first + ahead, end);
+  for (int t0 = first; t0 < end; t0 += STEP) {
+    const int tw = t0 + ahead;
+    if (t0 + STEP < end) nxt.load(a, l, u, gate, done, tw + STEP, end);
+    if constexpr (MODE == SCAN_FOLD || (!PARTS && S > 1)) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        VT A = VT::one(), B = VT::zero();
-        bool cut = false;
+      for (int k = 0; k < SCAN_K; ++k)
+        if (tw + k < end) {
+          const bool c = cur.done[k] != 0;
 #pragma unroll
-        for (int k = 0; k < SCAN_K; ++k)
-          if (tw + k < end) {
+          for (int v = 0; v < V; ++v) {
             const VT ak = [&] { if constexpr (DIAG) return lam[v]; else return cur.g[k].get(v); }();
             const VT uk = cur.u[k].get(v);
-            const bool c = cur.done[k] != 0;
-            B = c ? uk : VT::fma(ak, B, uk);
-            A = VT::mul(ak, A);
-            cut |= c;
+            B[v] = c ? uk : VT::fma(ak, B[v], uk);
+            A[v] = VT::mul(ak, A[v]);
           }
-        mine[v] = folded<DIAG>(A, B, cut);
-      }
-      if constexpr (AGG) {
-        ex.share(buf, w, lane, mine);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int j = 0; j < S; ++j) all[v] = ex.m[buf][j][v][lane].after(all[v]);
-      } else {
-        ex(buf, w, lane, mine, carry, into);
-      }
-      buf ^= 1;
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) into[v] = carry[v];
+          cut |= c;
+        }
     }
-    if constexpr (!AGG) {
+    if constexpr (MODE != SCAN_FOLD) {
+      if constexpr (!PARTS && S > 1) {
+        Map<DIAG> mine[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) mine[v] = folded<DIAG>(A[v], B[v], cut);
+        ex(buf, w, lane, mine, carry, into);
+        buf ^= 1;
+        restart();
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) into[v] = carry[v];
+      }
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k)
         if (tw + k < end) {
@@ -358,20 +404,21 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u,
           }
           if (h && l.live) store_vals<DT, DIAG, V>(h, l, tw + k, a.W, into);
         }
-      if constexpr (S == 1) {
+      if constexpr (PARTS || S == 1) {
 #pragma unroll
         for (int v = 0; v < V; ++v) carry[v] = into[v];
       }
     }
     cur = nxt;
   }
-  if constexpr (AGG) {
-    if (w == 0 && l.live)
+  if constexpr (MODE == SCAN_FOLD) {
+    Map<DIAG> mine[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, g + 1)[l.c + v] = all[v];
+    for (int v = 0; v < V; ++v) mine[v] = folded<DIAG>(A[v], B[v], cut);
+    leave_part<DIAG, V, S>(ws, N, gridDim.y, g, w, lane, l, ex, mine);
   } else if (h_last && end == a.T) {
-    states_read<S>();
-    if (w != 0 || !l.live) return;
+    if constexpr (!PARTS) states_read<S>();
+    if (!l.live || (PARTS ? first >= end : w != 0)) return;  // (the wave with the last step; any knows the state)
     if (done && done[(size_t)(a.T - 1) * a.E + l.env] != 0)
 #pragma unroll
       for (int v = 0; v < V; ++v) carry[v] = VT::zero();
@@ -404,7 +451,7 @@ struct BackBlock {
   }
 };
 
-template <int DT, bool DIAG, int V, int S, bool AGG, bool GRAD>
+template <int DT, bool DIAG, int V, int S, int MODE, bool GRAD>
 __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void* gate, const uint8_t* done,
                                                           const float* h0, const void* h, const void* dh,
                                                           const float* dh_last, void* du, void* dgate, float* dh0,
@@ -415,65 +462,69 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
   const size_t N = (size_t)a.E * a.A * a.W;
   const Lane<DIAG, V> l(a, lane, scan_block<S>(N * (DIAG ? 2 : 1) * elem_bytes<DT>()));
   const int g = blockIdx.y;
-  const int first = g * seg, end = a.T - first < seg ? a.T : first + seg;
+  constexpr bool PARTS = MODE != SCAN_WHOLE;
+  const int first = PARTS ? g * seg + w * (seg / S) : 0;
+  const int end = PARTS && a.T - first > seg / S ? first + seg / S : a.T;
+  constexpr int STEP = PARTS ? SCAN_K : S * SCAN_K;
   VT lam[V], carry[V], into[V], start[V];
   load_lambda<DT, DIAG, V>(gate, l, a.W, lam);
   if constexpr (GRAD) load_state<DIAG, V>(h0, l, a.W, start);
-  int buf = 0;
-  if (AGG || !ws) {
+  if constexpr (MODE == SCAN_PARTS) {
+    enter_part<DIAG, V, S>(ws, N, gridDim.y, g, w, lane, l, ex, carry);
+  } else {
     const bool ended = done && done[(size_t)(a.T - 1) * a.E + l.env] != 0;
     load_state<DIAG, V>(ended ? nullptr : dh_last, l, a.W, carry);
-    if (AGG && g == 0 && w == 0 && l.live)
+    if (MODE == SCAN_FOLD && g == 0 && w == 0 && l.live)
 #pragma unroll
       for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
-  } else {
-    enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
-    buf = 1;
   }
-  Map<DIAG> all[V];
+  VT A[V], B[V];
+  bool cut = false;
+  auto restart = [&]() {
 #pragma unroll
-  for (int v = 0; v < V; ++v) all[v] = {VT::one(), VT::zero()};
+    for (int v = 0; v < V; ++v) {
+      A[v] = VT::one();
+      B[v] = VT::zero();
+    }
+    cut = false;
+  };
+  restart();
   double sx[V], sy[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) sx[v] = sy[v] = 0.;
-
+  int buf = 0;
   BackBlock<DT, DIAG, V, GRAD> cur, nxt;
-  cur.load(a, l, dh, gate, h, done, first + w * SCAN_K, end);
-  for (int r0 = first; r0 < end; r0 += S * SCAN_K) {
-    const int rw = r0 + w * SCAN_K;
-    if (r0 + S * SCAN_K < end) nxt.load(a, l, dh, gate, h, done, rw + S * SCAN_K, end);
-    if constexpr (S > 1) {
-      Map<DIAG> mine[V];
+  const int ahead = PARTS ? 0 : w * SCAN_K;
+  cur.load(a, l, dh, gate, h, done, first + ahead, end);
+  for (int r0 = first; r0 < end; r0 += STEP) {
+    const int rw = r0 + ahead;
+    if (r0 + STEP < end) nxt.load(a, l, dh, gate, h, done, rw + STEP, end);
+    if constexpr (MODE == SCAN_FOLD || (!PARTS && S > 1)) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        VT A = VT::one(), B = VT::zero();
-        bool cut = false;
+      for (int k = 0; k < SCAN_K; ++k)
+        if (rw + k < end) {
+          const bool c = cur.done[k] != 0;
 #pragma unroll
-        for (int k = 0; k < SCAN_K; ++k)
-          if (rw + k < end) {
+          for (int v = 0; v < V; ++v) {
             const VT ak = [&] { if constexpr (DIAG) return lam[v].conj(); else return cur.g[k].get(v); }();
-            const bool c = cur.done[k] != 0;
-            B = c ? VT::zero() : VT::mul(ak, VT::add(cur.dh[k].get(v), B));
-            A = VT::mul(ak, A);
-            cut |= c;
+            B[v] = c ? VT::zero() : VT::mul(ak, VT::add(cur.dh[k].get(v), B[v]));
+            A[v] = VT::mul(ak, A[v]);
           }
-        mine[v] = folded<DIAG>(A, B, cut);
-      }
-      if constexpr (AGG) {
-        ex.share(buf, w, lane, mine);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int j = 0; j < S; ++j) all[v] = ex.m[buf][j][v][lane].after(all[v]);
-      } else {
-        ex(buf, w, lane, mine, carry, into);
-      }
-      buf ^= 1;
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) into[v] = carry[v];
+          cut |= c;
+        }
     }
-    if constexpr (!AGG) {
+    if constexpr (MODE != SCAN_FOLD) {
+      if constexpr (!PARTS && S > 1) {
+        Map<DIAG> mine[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) mine[v] = folded<DIAG>(A[v], B[v], cut);
+        ex(buf, w, lane, mine, carry, into);
+        buf ^= 1;
+        restart();
+      } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) into[v] = carry[v];
+      }
       float fx[V], fy[V];  // this block's part of the sums over steps
 #pragma unroll
       for (int v = 0; v < V; ++v) fx[v] = fy[v] = 0.f;
@@ -505,7 +556,7 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
         }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if constexpr (S == 1) carry[v] = into[v];
+        if constexpr (PARTS || S == 1) carry[v] = into[v];
         if constexpr (GRAD && DIAG) {
           sx[v] += (double)fx[v];
           sy[v] += (double)fy[v];
@@ -514,14 +565,15 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
     }
     cur = nxt;
   }
-  if constexpr (AGG) {
-    if (w == 0 && l.live)
+  if constexpr (MODE == SCAN_FOLD) {
+    Map<DIAG> mine[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, g + 1)[l.c + v] = all[v];
+    for (int v = 0; v < V; ++v) mine[v] = folded<DIAG>(A[v], B[v], cut);
+    leave_part<DIAG, V, S>(ws, N, gridDim.y, g, w, lane, l, ex, mine);
   } else {
     if (dh0 && end == a.T) {
-      states_read<S>();
-      if (w == 0 && l.live) store_state<DIAG, V>(dh0, l, a.W, carry);
+      if constexpr (!PARTS) states_read<S>();
+      if (l.live && (PARTS ? first < end : w == 0)) store_state<DIAG, V>(dh0, l, a.W, carry);
     }
     if constexpr (GRAD && DIAG) {
       // the waves' sums in order, then one partial sum per channel and segment
@@ -607,7 +659,7 @@ ScanPlan scan_plan(const ScanArgs& p) {
 size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t slot_bytes(const ScanArgs& p, const ScanPlan& s) {
   if (s.G == 1) return 0;
-  return round256((size_t)(s.G + 1) * p.E * p.A * p.W * (p.diag ? sizeof(Map<true>) : sizeof(Map<false>)));
+  return round256((size_t)(s.G + 1 + s.G * s.S) * p.E * p.A * p.W * (p.diag ? sizeof(Map<true>) : sizeof(Map<false>)));
 }
 
 // Two bfloat16 channels to a lane where rows have an even number of them and
@@ -629,11 +681,14 @@ template <int DT, bool DIAG, int V, int S>
 void run_scan(const ScanArgs& p, const ScanPlan& pl, const void* u, const void* gate, const uint8_t* done,
               const float* h0, void* h, float* h_last, void* ws, hipStream_t s) {
   if constexpr (S == 8)  // (segments are taken with 8 waves)
-    if (pl.G > 1)
-      scan_kernel<DT, DIAG, V, S, true><<<scan_grid(p, V, pl.G - 1), 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last,
-                                                                                     ws, pl.seg);
-  scan_kernel<DT, DIAG, V, S, false><<<scan_grid(p, V, pl.G), 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last,
-                                                                              pl.G > 1 ? ws : nullptr, pl.seg);
+    if (pl.G > 1) {
+      const dim3 grid = scan_grid(p, V, pl.G);
+      scan_kernel<DT, DIAG, V, S, SCAN_FOLD><<<grid, 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last, ws, pl.seg);
+      scan_kernel<DT, DIAG, V, S, SCAN_PARTS><<<grid, 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last, ws, pl.seg);
+      return;
+    }
+  scan_kernel<DT, DIAG, V, S, SCAN_WHOLE><<<scan_grid(p, V, 1), 64 * S, 0, s>>>(p, u, gate, done, h0, h, h_last, ws,
+                                                                                pl.seg);
 }
 
 template <int DT, bool DIAG, int V, int S, bool GRAD>
@@ -641,12 +696,19 @@ void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const
                   const void* h, const void* dh, const float* dh_last, void* du, void* dgate, float* dh0, void* ws,
                   hipStream_t s) {
   double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + slot_bytes(p, pl));
+  const dim3 grid = scan_grid(p, V, pl.G);
+  bool parts = false;
   if constexpr (S == 8)
-    if (pl.G > 1)
-      scan_bwd_kernel<DT, DIAG, V, S, true, false><<<scan_grid(p, V, pl.G - 1), 64 * S, 0, s>>>(
-          p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, ws, part, pl.seg);
-  scan_bwd_kernel<DT, DIAG, V, S, false, GRAD><<<scan_grid(p, V, pl.G), 64 * S, 0, s>>>(
-      p, gate, done, h0, h, dh, dh_last, du, dgate, dh0, pl.G > 1 ? ws : nullptr, part, pl.seg);
+    if (pl.G > 1) {
+      parts = true;
+      scan_bwd_kernel<DT, DIAG, V, S, SCAN_FOLD, false><<<grid, 64 * S, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
+                                                                               dgate, dh0, ws, part, pl.seg);
+      scan_bwd_kernel<DT, DIAG, V, S, SCAN_PARTS, GRAD><<<grid, 64 * S, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
+                                                                               dgate, dh0, ws, part, pl.seg);
+    }
+  if (!parts)
+    scan_bwd_kernel<DT, DIAG, V, S, SCAN_WHOLE, GRAD><<<grid, 64 * S, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
+                                                                             dgate, dh0, ws, part, pl.seg);
   if (DIAG && GRAD)
     scan_dlam_kernel<<<dim3((unsigned)((p.W + RED_P - 1) / RED_P), 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
                                                                static_cast<float*>(dgate));
