@@ -632,7 +632,8 @@ __global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, i
 //     room for a second workgroup (250 x 32768: 19 against 25).  Complex maps
 //     cost more to exchange: 8 is as good or better there at every size;
 //   * segments read the inputs twice, and pay where workgroups leave most CUs
-//     idle (2000 x 4096: 32 in 8 segments, 50 in one; 2000 x 8192: 55 and 55).
+//     idle (2000 x 4096: 31 in 8 segments, 55 in one; 2000 x 8192: 61 in 4, 71;
+//     2000 x 16384: 140 in 2, 88; 500 x 4096: 14 in 3, 17).
 struct ScanPlan {
   int S, G, seg;
 };
@@ -647,7 +648,7 @@ ScanPlan scan_plan(const ScanArgs& p) {
   }
   const int block = 8 * SCAN_K;
   const int64_t want = (512 + waves - 1) / waves, most = p.T / (2 * block), g = want < most ? want : most;
-  if (waves <= 128 && g >= 4) {
+  if (waves <= 128 && g >= 2) {
     s.S = 8;
     s.seg = (int)(((p.T + g - 1) / g + block - 1) / block * block);
     s.G = (p.T + s.seg - 1) / s.seg;
