@@ -749,6 +749,8 @@ def ppo_loss(logits, actions, logp_old, adv, value, ret, clip=0.2, value_coef=0.
     stats), stats [6] named by PPO_STATS.  ``workspace``: uint8, at least ppo_workspace_bytes(logits) bytes
     (allocated when None)."""
     dev, shape = _lead(logits, "logits"), logits.shape
+    if len(shape) == 0:
+        raise ValueError("logits must be [.., nA]")
     lead, na = shape[:-1], shape[-1]
     f32, u8 = torch.float32, torch.uint8
     cfg = _PpoConfig(lead.numel(), na, int(normalize), clip, value_clip, value_coef, entropy_coef)
