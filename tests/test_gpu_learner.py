@@ -663,7 +663,7 @@ def test_binding_checks_on_the_gpu():
                 lambda: R.scan(u, z(4, 2, 2, 8), workspace=z(16)),
                 lambda: R.scan_backward(u, z(4, 2, 2, 8), z(4, 2, 2, 8), dh0=z(2, 2, 9)),
                 lambda: R.ppo_loss(z(5, 6), z(5), z(5), z(5), z(5), z(5)),
-                lambda: R.ppo_loss(z(), z(dt=torch.int32), z(), z(), z(), z()),
+                lambda: R.ppo_loss(z(1)[0], z(1, dt=torch.int32), *[z(1)] * 4),
                 lambda: R.ppo_loss(z(5, 6), z(4, dt=torch.int32), z(5), z(5), z(5), z(5)),
                 lambda: R.ppo_loss(z(5, 6), z(5, dt=torch.int32), z(5), z(5), z(5), z(5), stats=z(5)),
                 lambda: R.orthogonalize(z(4, 6).t()), lambda: R.orthogonalize(z(4, 6), out=z(6, 4))):
