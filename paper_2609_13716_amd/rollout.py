@@ -612,6 +612,8 @@ def _arg(t, name, dtype, shape, dev):
     shape."""
     if t is None:
         return None
+    if t.get_device() == dev and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return t.data_ptr()
     if t.get_device() != dev:
         raise ValueError(f"{name} must be a device tensor" if not t.is_cuda else
                          f"{name} is on {t.device}, the call's first tensor on cuda:{dev}")
@@ -619,9 +621,7 @@ def _arg(t, name, dtype, shape, dev):
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _on(stream, dev):
@@ -768,15 +768,20 @@ def ppo_loss(logits, actions, logp_old, adv, value, ret, clip=0.2, value_coef=0.
                 _arg(value, "value", f32, lead, dev), _arg(value_old, "value_old", f32, lead, dev),
                 _arg(ret, "ret", f32, lead, dev), _arg(dlogits, "dlogits", f32, shape, dev),
                 _arg(dvalue, "dvalue", f32, lead, dev), _arg(stats, "stats", f32, (6,), dev))
-        keep, ws, n = _workspace(workspace, lib.rl_ppo_workspace_bytes(ref), dev)
+        keep, ws, n = _workspace(workspace, _ppo_need(cfg.n_rows, na), dev)
         _check(lib.rl_ppo_loss(ref, *args, ws, n, _raw_stream(dev)))
     return dlogits, dvalue, stats
 
 
+@functools.lru_cache(maxsize=1024)
+def _ppo_need(rows, na):
+    """Workspace bytes of a loss over so many rows, by its sizes alone (0 for sizes that the call will refuse)."""
+    return lib.rl_ppo_workspace_bytes(ctypes.byref(_PpoConfig(rows, na, 0, 0.2, 0.0, 0.0, 0.0)))
+
+
 def ppo_workspace_bytes(logits):
     """Bytes of workspace ppo_loss needs for these logits."""
-    cfg = _PpoConfig(logits.shape[:-1].numel(), logits.shape[-1], 0, 0.2, 0.0, 0.0, 0.0)
-    return lib.rl_ppo_workspace_bytes(ctypes.byref(cfg))
+    return _ppo_need(logits.shape[:-1].numel(), logits.shape[-1])
 
 
 def _ortho_sizes(g):
