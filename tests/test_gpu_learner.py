@@ -560,6 +560,47 @@ def test_orthogonalize_special_matrices(size):
     _check_ortho(big, R.orthogonalize(big))
 
 
+# ---- beyond 32-bit offsets ----
+
+
+def test_scan_beyond_32_bits():
+    """5 GB of values: after an episode's end in every env the last steps are those of a call of their own, and before
+    the first end the first steps' gradients are, too."""
+    T, E, A, W, n = 40000, 64, 2, 512, 3000
+    g = torch.Generator(device="cuda").manual_seed(14)
+    u = torch.randn(T, E, A, W, generator=g, device="cuda", dtype=torch.bfloat16)
+    gate = torch.rand(T, E, A, W, generator=g, device="cuda", dtype=torch.bfloat16)
+    assert u.numel() > 2 ** 31
+    done = torch.zeros(T, E, dtype=torch.uint8, device="cuda")
+    done[T - n - 1] = 1
+    done[n - 1] = 1
+    h, last = R.scan(u, gate, done)
+    tail, tail_last = R.scan(u[T - n:], gate[T - n:], done[T - n:])
+    assert torch.allclose(h[T - n:].float(), tail.float(), rtol=2 ** -7, atol=2 ** -16)
+    assert torch.allclose(last, tail_last, rtol=1e-5, atol=1e-5)
+    assert torch.equal(h[n], u[n]) and torch.equal(h[T - n], u[T - n])
+    du, dgate, _ = R.scan_backward(gate, h, u, done)
+    for a, b in ((0, n), (T - n, T)):
+        part = R.scan_backward(gate[a:b], h[a:b], u[a:b], done[a:b])
+        assert torch.allclose(du[a:b].float(), part[0].float(), rtol=2 ** -7, atol=2 ** -16)
+        assert torch.allclose(dgate[a:b].float(), part[1].float(), rtol=2 ** -6, atol=2 ** -12)
+
+
+def test_ppo_beyond_32_bits():
+    """2.2 G logits: the last rows' gradients are those of a call of their own, but for the number of rows."""
+    R_, nA, n = 110_000_000, 20, 5000
+    g = torch.Generator(device="cuda").manual_seed(15)
+    x = torch.randn(R_, nA, generator=g, device="cuda")
+    f = [torch.randn(R_, generator=g, device="cuda") for _ in range(4)]
+    act = torch.randint(0, nA, (R_,), generator=g, device="cuda", dtype=torch.int32)
+    dx, dv, st = R.ppo_loss(x, act, f[0] - 3, f[1], f[2], f[3])
+    px, pv, _ = R.ppo_loss(x[-n:], act[-n:], f[0][-n:] - 3, f[1][-n:], f[2][-n:], f[3][-n:])
+    # 1 / rows is rounded once more in each
+    assert torch.allclose(dx[-n:].double() * R_, px.double() * n, rtol=2 ** -22, atol=2 ** -22)
+    assert torch.allclose(dv[-n:].double() * R_, pv.double() * n, rtol=2 ** -22)
+    assert bool(torch.isfinite(st).all())
+
+
 # ---- streams, graphs, repeated calls ----
 
 
