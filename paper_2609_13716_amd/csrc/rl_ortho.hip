@@ -17,7 +17,7 @@
 // Layout.  Operands lie in the workspace as the matrix instruction reads
 // them: for 32 rows and 16 columns 1 KB holds lane l's 8 values (row l % 32,
 // columns 8 (l / 32) ..), hi followed by lo, so a wave's operand load is 1 KB
-// contiguous and needs no LDS.  X is stored once by rows (for X X^T) and once
+// contiguous, from memory or from LDS.  X is stored once by rows (for X X^T) and once
 // by columns (for B X, whose sum runs over X's rows); A and B are symmetric,
 // so only tiles on and below the diagonal are computed and written twice.
 #include "rl_internal.h"

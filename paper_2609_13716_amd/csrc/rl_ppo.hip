@@ -5,8 +5,8 @@
 // busy for about as long.  A wave takes 64 consecutive rows: their 64 nA logits
 // are read as 16 nA pieces of 16 bytes and turned into one row per lane through
 // LDS (illegal actions become -inf on the way), the row stays in registers, and
-// the gradients go back the same way.  1048576 rows of 6 take 29 us, 20 of them
-// for the rows (4.1 TB/s), the rest for the two other launches.
+// the gradients go back the same way.  1048576 rows of 6 take 28 us, 20 of them
+// for the rows (4.0 TB/s), the rest for the two other launches.
 // Sums over rows are float64, taken in an order that depends on the sizes only:
 // per lane, wave, workgroup, then over workgroups by the launch that follows.
 //   R <= PPO_SMALL   one workgroup does everything in one launch (500 rows of
@@ -21,7 +21,7 @@ namespace rl {
 namespace {
 
 constexpr int PPO_NT = 512;         // threads of a workgroup that does rows
-constexpr int PPO_SUM_NT = 1024;    // of one that adds up advantages
+constexpr int PPO_SUM_NT = 512;     // of one that adds up advantages
 constexpr int64_t PPO_SMALL = 2048;
 constexpr int PPO_ADV_B = 64, PPO_ROW_B = 512;  // workgroups, at most (their partial sums go to the workspace)
 constexpr int PPO_STATS = 6;
@@ -101,6 +101,39 @@ __device__ __forceinline__ void adv_sums(const PpoArgs& p, double shift, int64_t
     v[1] += a;
     v[2] += a * a;
   }
+}
+
+// The same, four neighbouring rows at a time, ADV_U times that in flight;
+// false (and nothing done) where the arrays are not aligned to that.
+constexpr int ADV_U = 4;
+__device__ __forceinline__ bool adv_sums4(const PpoArgs& p, double shift, int64_t first, int64_t step, double (&v)[3]) {
+  if ((reinterpret_cast<uintptr_t>(p.adv) & 15) | (reinterpret_cast<uintptr_t>(p.mask) & 3)) return false;
+  const int64_t fours = p.R / 4;
+  auto add = [&](bool in, float read) {
+    const double a = in ? (double)read - shift : 0.;
+    v[0] += in ? 1. : 0.;
+    v[1] += a;
+    v[2] += a * a;
+  };
+  for (int64_t r = first; r < fours; r += ADV_U * step) {
+    f32x4 a[ADV_U];
+    uint32_t in[ADV_U];
+#pragma unroll
+    for (int q = 0; q < ADV_U; ++q) {
+      const int64_t at = r + q * step < fours ? r + q * step : r;  // (past the last ones: read again, not counted)
+      a[q] = reinterpret_cast<const f32x4*>(p.adv)[at];
+      in[q] = p.mask ? reinterpret_cast<const uint32_t*>(p.mask)[at] : 0x01010101u;
+    }
+#pragma unroll
+    for (int q = 0; q < ADV_U; ++q) {
+      if (r + q * step >= fours) in[q] = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) add(in[q] >> 8 * k & 255, a[q][k]);
+    }
+  }
+  const int64_t rest = 4 * fours + first;
+  if (rest < p.R) add(!p.mask || p.mask[rest], p.adv[rest]);
+  return true;
 }
 
 struct PpoNorm {
@@ -336,7 +369,8 @@ __global__ __launch_bounds__(PPO_SUM_NT) void ppo_adv_kernel(PpoArgs p, PpoPart*
   double v[3] = {0., 0., 0.};
   const double shift = p.normalize ? adv_shift(p) : 0.;
   if (blockIdx.x == 0 && threadIdx.x == 0) part->shift = shift;
-  adv_sums(p, shift, (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, (int64_t)gridDim.x * PPO_SUM_NT, v);
+  const int64_t first = (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, step = (int64_t)gridDim.x * PPO_SUM_NT;
+  if (!adv_sums4(p, shift, first, step, v)) adv_sums(p, shift, first, step, v);
   block_sum<3>(v, s);
   if (threadIdx.x == 0)
     for (int i = 0; i < 3; ++i) part->adv[blockIdx.x][i] = v[i];
@@ -350,7 +384,7 @@ __host__ __device__ constexpr int ppo_wave_bytes(int na) {
 
 // Up to 20 actions the registers are held to what four waves of a SIMD may
 // have (two workgroups to a CU; at 20 that spills 8 dwords: 655361 masked rows
-// 45 us, 51 without); beyond, too much would be spilled (400000 rows of 24: 52
+// 41 us, 47 without); beyond, too much would be spilled (400000 rows of 24: 52
 // us, 42 without).
 template <int NA>
 __global__ __launch_bounds__(PPO_NT, NA <= 20 ? 4 : 1) void ppo_rows_kernel(PpoArgs p, PpoPart* part, int adv_blocks) {
@@ -432,7 +466,7 @@ hipError_t run_ppo(const PpoArgs& p, void* workspace, hipStream_t s) {
   }
   PpoPart* part = static_cast<PpoPart*>(workspace);
   const int nt = wave * (PPO_NT / 64) > 62 * 1024 ? PPO_NT / 2 : PPO_NT;  // (a workgroup has 64 KB of LDS)
-  const int64_t tiles = (p.R + nt - 1) / nt, sums = (p.R + PPO_SUM_NT - 1) / PPO_SUM_NT;
+  const int64_t tiles = (p.R + nt - 1) / nt, sums = (p.R + 4 * PPO_SUM_NT - 1) / (4 * PPO_SUM_NT);
   const int blocks = (int)(tiles < PPO_ROW_B ? tiles : PPO_ROW_B);
   const int adv_blocks = p.normalize || p.mask ? (int)(sums < PPO_ADV_B ? sums : PPO_ADV_B) : 0;
   if (adv_blocks) ppo_adv_kernel<<<adv_blocks, PPO_SUM_NT, 0, s>>>(p, part);
