@@ -637,7 +637,7 @@ rl_status rl_scan_backward(const rl_scan_config* cfg, const void* gate, const ui
 size_t rl_ppo_workspace_bytes(const rl_ppo_config* cfg) {
   if (check_ppo(cfg) != RL_OK) return 0;
   ok();
-  return rl::ppo_workspace_bytes(cfg->n_rows);
+  return rl::ppo_workspace_bytes(cfg->n_rows, cfg->n_actions);
 }
 
 rl_status rl_ppo_loss(const rl_ppo_config* cfg, const float* logits, const uint8_t* legal, const uint8_t* mask,
@@ -657,7 +657,7 @@ rl_status rl_ppo_loss(const rl_ppo_config* cfg, const float* logits, const uint8
   const void* words[] = {logits, actions, logp_old, adv, value, value_old, ret, dlogits, dvalue, stats};
   for (const void* w : words)
     if (!aligned_to(w, 4)) return fail(RL_EINVAL, "an array is not aligned to its elements");
-  const size_t need = rl::ppo_workspace_bytes(cfg->n_rows);
+  const size_t need = rl::ppo_workspace_bytes(cfg->n_rows, cfg->n_actions);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
     return fail(RL_EINVAL, "workspace needs %zu bytes, 16-byte aligned (got %zu)", need, workspace_bytes);
   const rl::PpoArgs p{cfg->n_rows, cfg->n_actions, cfg->normalize_adv, cfg->clip, cfg->value_clip, cfg->value_coef,

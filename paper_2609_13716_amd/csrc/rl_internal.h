@@ -297,7 +297,7 @@ struct PpoArgs {
   float* dvalue;
   float* stats;
 };
-size_t ppo_workspace_bytes(int64_t R);
+size_t ppo_workspace_bytes(int64_t R, int na);
 hipError_t launch_ppo(const PpoArgs& p, void* workspace, hipStream_t s);
 
 // Newton-Schulz orthogonalisation (rl_ortho.hip).

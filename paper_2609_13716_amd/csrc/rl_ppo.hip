@@ -9,7 +9,7 @@
 // for the rows (4.0 TB/s), the rest for the two other launches.
 // Sums over rows are float64, taken in an order that depends on the sizes only:
 // per lane, wave, workgroup, then over workgroups by the launch that follows.
-//   R <= PPO_SMALL   one workgroup does everything in one launch (500 rows of
+//   few rows         one workgroup does everything in one launch (500 rows of
 //                    6: 7 us of GPU time; 15 in three launches);
 //   otherwise        the advantages' sums (when they are normalised or rows
 //                    masked out), the rows, the six means.
@@ -22,7 +22,10 @@ namespace {
 
 constexpr int PPO_NT = 512;         // threads of a workgroup that does rows
 constexpr int PPO_SUM_NT = 512;     // of one that adds up advantages
-constexpr int64_t PPO_SMALL = 2048;
+// Whether one workgroup does everything.  Its time grows with rows and actions;
+// three launches take 15.7 us whatever there is to do (rows of 6: 2000 11.6 us,
+// 3800 17.2; of 9: 2000 14.2, 2800 17.3; of 32: 1024 14.8, 1200 20.8).
+inline bool ppo_small(int64_t R, int na) { return R * (na + 8) <= 40 * 1024; }
 constexpr int PPO_ADV_B = 64, PPO_ROW_B = 512;  // workgroups, at most (their partial sums go to the workspace)
 constexpr int PPO_STATS = 6;
 
@@ -457,7 +460,7 @@ __global__ __launch_bounds__(PPO_NT) void ppo_small_kernel(PpoArgs p) {
 template <int NA>
 hipError_t run_ppo(const PpoArgs& p, void* workspace, hipStream_t s) {
   const size_t wave = ppo_wave_bytes(NA);
-  if (p.R <= PPO_SMALL) {
+  if (ppo_small(p.R, NA)) {
     const int most = (int)((60u << 10) / wave), rows = (int)((p.R + 63) / 64);  // waves that fit in LDS; row tiles
     const int waves = rows < most ? rows : most;
     const int n = waves < PPO_NT / 64 ? waves : PPO_NT / 64;
@@ -483,7 +486,7 @@ hipError_t pick_ppo(std::integer_sequence<int, N...>, const PpoArgs& p, void* wo
 
 }  // namespace
 
-size_t ppo_workspace_bytes(int64_t R) { return R <= PPO_SMALL ? 0 : sizeof(PpoPart); }
+size_t ppo_workspace_bytes(int64_t R, int na) { return ppo_small(R, na) ? 0 : sizeof(PpoPart); }
 
 hipError_t launch_ppo(const PpoArgs& p, void* workspace, hipStream_t s) {
   return pick_ppo(std::make_integer_sequence<int, MAX_NA>(), p, workspace, s);
