@@ -201,10 +201,15 @@ __device__ __forceinline__ double exp64(double x) {
 // multiple of 8 (whose 64 starts would share few banks) are 4 floats apart.
 __host__ __device__ constexpr int ppo_ld(int na) { return na % 8 == 0 ? na + 4 : na; }
 
-// A logit less the row's largest; far below zero for an illegal action (so
-// that its probability is 0 and a product with it is, too).
-constexpr float FAR_BELOW = -1e30f;
-__device__ __forceinline__ float below_top(float x, float top) { return x == -INFINITY ? FAR_BELOW : x - top; }
+// A logit less the row's largest, no lower than LEAST, whose exponential is 0
+// in float32 already: the probability of a logit at float32's lowest value (or
+// so far from the largest that the difference overflows) is 0, and so are
+// products with it.  FAR_BELOW, lower still, stands for an illegal action.
+constexpr float FAR_BELOW = -1e30f, LEAST = -200.f;
+__device__ __forceinline__ float below_top(float x, float top) {
+  const float d = x - top;  // (a NaN stays one)
+  return x == -INFINITY ? FAR_BELOW : d < LEAST ? LEAST : d;
+}
 
 // A lane's row in LDS -> registers, and back, by the widest pieces that every
 // row is aligned to.
@@ -299,7 +304,8 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
   if (!(xa == -INFINITY)) {
     const float adv = (float)(((double)adv_in - nm.mean) * nm.rstd);
     const float lo = (float)(1. - (double)p.clip), hi = (float)(1. + (double)p.clip);
-    const float diff = xa - top - logs - old, ratio = exp32(diff > 200.f ? 200.f : diff < -200.f ? -200.f : diff);
+    const double diff64 = (double)xa - top - logs - old;  // (of float32 it may pass the range)
+    const float diff = (float)diff64, ratio = exp32(diff > 200.f ? 200.f : diff < -200.f ? -200.f : diff);
     bool below = ratio < lo, above = ratio > hi;
     // near a border the float32 ratio does not say on which side it lies (the borders' own rounding is within tol)
     const float tol = 1e-6f * (16.f + fabsf(xa) + fabsf(top) + fabsf(old)) * ratio;
@@ -317,7 +323,7 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     const bool plain = adv > 0.f ? !above : adv < 0.f ? !below : true;
     st[1] -= (double)((plain ? ratio : clipped) * adv);
     slope = plain ? -adv * ratio : 0.f;
-    st[4] += (double)(ratio - 1.f - diff);
+    st[4] += (double)ratio - 1. - diff64;
     st[5] += below || above ? 1. : 0.;
   }
   if (counted && some) st[3] += (double)ent;
