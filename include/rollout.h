@@ -267,11 +267,12 @@ rl_status rl_gae(const float* reward, const uint8_t* done, const float* value, c
  * T = 1 with h_last in h0's place is one step of a policy that acts.
  * Values (u, gate, h and their gradients) are float32 or bfloat16; states
  * (h0, h_last, dh0, dh_last), lambda_bar and its gradient are float32, and the
- * recurrence runs in float32.  Long runs of few rows are cut into segments
- * that are folded as affine maps, so T steps in one call and in two agree to
- * rounding, not to the bit; gates are expected not to let the product of
- * a segment's gates overflow float32 (|a| <= 1 never does).  Equal calls give equal
- * bits.
+ * recurrence runs in float32.  Runs of few rows are cut into parts that are
+ * folded as affine maps, so T steps in one call and in two agree to rounding,
+ * not to the bit.  Factors may have any finite size (products of them are
+ * carried in float64): h_t is right to rounding of S_t = sum_j |a_t .. a_{j+1}|
+ * |u_j|, its episode's terms and h0's, where S fits float32 up to that step.
+ * Equal calls give equal bits.
  * Limits: sizes >= 1; n_steps <= 2^30; n_envs * n_agents * width (twice that
  * for RL_SCAN_DIAGONAL) < 2^31. */
 enum { RL_SCAN_GATED = 0, RL_SCAN_DIAGONAL = 1 };

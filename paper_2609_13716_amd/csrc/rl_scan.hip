@@ -21,6 +21,11 @@
 //     second (inputs are read twice).
 // Episode ends cut the state: a map that contains one does not read its input.
 // It is marked by SCAN_CUT in place of A, so that 0 * NaN never arises.
+// A map's A is a product of factors, which may leave float32's range and come
+// back, or grow while the states are 0, where every state fits: it is float64,
+// held within 2^500 (a larger one meets a state of 0, or makes an infinity of
+// any other float32 anyway; and four factors below 2^128 may follow before the
+// next check).
 #include <initializer_list>
 
 #include "rl_internal.h"
@@ -29,7 +34,8 @@ namespace rl {
 namespace {
 
 constexpr int SCAN_K = 8;           // steps a wave holds in registers
-constexpr uint32_t SCAN_CUT = 0x7fc0dead;  // a NaN that stands for "the state before is cut off"
+constexpr int SCAN_CUT = 0x7ff8dead;  // upper half of a NaN that stands for "the state before is cut off"
+constexpr double SCAN_MOST = 0x1p500;
 
 // A channel's value: one float, or a complex number.
 template <bool DIAG>
@@ -38,7 +44,6 @@ template <>
 struct Val<false> {
   float x;
   __device__ static Val zero() { return {0.f}; }
-  __device__ static Val one() { return {1.f}; }
   __device__ static Val add(Val a, Val b) { return {a.x + b.x}; }
   __device__ static Val mul(Val a, Val b) { return {a.x * b.x}; }
   __device__ static Val fma(Val a, Val h, Val u) { return {fmaf(a.x, h.x, u.x)}; }
@@ -48,7 +53,6 @@ template <>
 struct Val<true> {
   float x, y;
   __device__ static Val zero() { return {0.f, 0.f}; }
-  __device__ static Val one() { return {1.f, 0.f}; }
   __device__ static Val add(Val a, Val b) { return {a.x + b.x, a.y + b.y}; }
   __device__ static Val mul(Val a, Val b) { return {fmaf(a.x, b.x, -a.y * b.y), fmaf(a.x, b.y, a.y * b.x)}; }
   __device__ static Val fma(Val a, Val h, Val u) {
@@ -57,34 +61,84 @@ struct Val<true> {
   __device__ Val conj() const { return {x, -y}; }
 };
 
+__device__ __forceinline__ double bounded(double x) { return fabs(x) > SCAN_MOST ? copysign(SCAN_MOST, x) : x; }
+
+// The same in float64: products of factors, and a state on its way through maps.
+template <bool DIAG>
+struct Wide;
+template <>
+struct Wide<false> {
+  double x;
+  __device__ static Wide one() { return {1.}; }
+  __device__ static Wide of(Val<false> v) { return {(double)v.x}; }
+  __device__ static Wide mul(Wide a, Wide b) { return {a.x * b.x}; }
+  __device__ static Wide fma(Wide a, Wide h, Val<false> u) { return {::fma(a.x, h.x, (double)u.x)}; }
+  __device__ Wide held() const { return {bounded(x)}; }
+  __device__ Val<false> val() const { return {(float)x}; }
+};
+template <>
+struct Wide<true> {
+  double x, y;
+  __device__ static Wide one() { return {1., 0.}; }
+  __device__ static Wide of(Val<true> v) { return {(double)v.x, (double)v.y}; }
+  __device__ static Wide mul(Wide a, Wide b) { return {::fma(a.x, b.x, -a.y * b.y), ::fma(a.x, b.y, a.y * b.x)}; }
+  __device__ static Wide fma(Wide a, Wide h, Val<true> u) {
+    return {::fma(a.x, h.x, ::fma(-a.y, h.y, (double)u.x)), ::fma(a.x, h.y, ::fma(a.y, h.x, (double)u.y))};
+  }
+  __device__ Wide held() const { return {bounded(x), bounded(y)}; }
+  __device__ Val<true> val() const { return {(float)x, (float)y}; }
+};
+
 // An affine map of the carried state, or (a cut one) a constant.
 template <bool DIAG>
 struct Map {
   using V = Val<DIAG>;
-  V a, b;
+  using W = Wide<DIAG>;
+  W a;
+  V b;
   __device__ static Map constant(V b) {
-    V a = V::zero();
-    a.x = __uint_as_float(SCAN_CUT);
+    W a = W::one();
+    a.x = __hiloint2double(SCAN_CUT, 0);
     return {a, b};
   }
-  __device__ bool cut() const { return __float_as_uint(a.x) == SCAN_CUT; }
-  __device__ V operator()(V h) const { return cut() ? b : V::fma(a, h, b); }
+  __device__ bool cut() const { return __double2hiint(a.x) == SCAN_CUT; }
+  __device__ W operator()(W h) const { return cut() ? W::of(b) : W::fma(a, h, b); }
   // this map after m
   __device__ Map after(const Map& m) const {
     if (cut()) return *this;
-    if (m.cut()) return constant(V::fma(a, m.b, b));
-    return {V::mul(a, m.a), V::fma(a, m.b, b)};
+    const V end = W::fma(a, W::of(m.b), b).val();
+    if (m.cut()) return constant(end);
+    return {W::mul(a, m.a).held(), end};
   }
 };
 
 // The map folded from steps with product a and end value b, of which one was
 // cut (or not): a product that happens to be the marker becomes another NaN.
 template <bool DIAG>
-__device__ __forceinline__ Map<DIAG> folded(Val<DIAG> a, Val<DIAG> b, bool cut) {
-  Map<DIAG> m{a, b};
+__device__ __forceinline__ Map<DIAG> folded(Wide<DIAG> a, Val<DIAG> b, bool cut) {
   if (cut) return Map<DIAG>::constant(b);
-  if (m.cut()) m.a.x = __uint_as_float(0x7fc00000u);
+  Map<DIAG> m{a.held(), b};
+  if (m.cut()) m.a.x = __hiloint2double(0x7ff80000, 0);
   return m;
+}
+
+// The product of a block's factors: gate after gate (k: its place in the
+// block), or the n-th power of one factor (p: the SCAN_K-th).
+__device__ __forceinline__ void take_gate(Wide<false>& a, Val<false> gate, int k) {
+  a = Wide<false>::mul(a, Wide<false>::of(gate));
+  if (k % 4 == 3) a = a.held();
+}
+__device__ __forceinline__ Wide<true> power(Val<true> lam) {
+  Wide<true> p = Wide<true>::of(lam);
+#pragma unroll
+  for (int k = 1; k < SCAN_K; k *= 2) p = Wide<true>::mul(p, p).held();
+  return p;
+}
+__device__ __forceinline__ Wide<true> power(Val<true> lam, Wide<true> p, int n) {
+  if (n >= SCAN_K) return p;
+  Wide<true> a = Wide<true>::one();
+  for (int k = 0; k < n; ++k) a = Wide<true>::mul(a, Wide<true>::of(lam)).held();
+  return a;
 }
 
 // The V neighbouring channels of a lane (of one row) at a step, as loaded:
@@ -200,10 +254,18 @@ __device__ __forceinline__ void store_state(float* base, const Lane<DIAG, V>& l,
 // between, which every wave reaches after reading b.
 template <bool DIAG, int V, int S>
 struct Exchange {
-  Map<DIAG> m[2][S][V][64];
+  // Maps read at a time: more of them hold registers that the gradients of complex channels do not have (128 steps x
+  // 65536 of them: 73 us with 4, 58 with 1), and gates have (2000 x 32768: 99 and 105 us).
+  static constexpr int TOGETHER = DIAG ? 1 : 4;
+  Wide<DIAG> a[2][S][V][64];
+  Val<DIAG> b[2][S][V][64];
+  __device__ Map<DIAG> map(int buf, int w, int v, int lane) const { return {a[buf][w][v][lane], b[buf][w][v][lane]}; }
   __device__ void share(int buf, int w, int lane, const Map<DIAG> (&mine)[V]) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) m[buf][w][v][lane] = mine[v];
+    for (int v = 0; v < V; ++v) {
+      a[buf][w][v][lane] = mine[v].a;
+      b[buf][w][v][lane] = mine[v].b;
+    }
     __syncthreads();
   }
   __device__ void operator()(int buf, int w, int lane, const Map<DIAG> (&mine)[V], Val<DIAG> (&carry)[V],
@@ -211,11 +273,14 @@ struct Exchange {
     share(buf, w, lane, mine);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
+      Wide<DIAG> c = Wide<DIAG>::of(carry[v]), at = c;
+#pragma unroll TOGETHER
       for (int j = 0; j < S; ++j) {
-        if (j == w) into[v] = carry[v];
-        carry[v] = m[buf][j][v][lane](carry[v]);
+        if (j == w) at = c;
+        c = map(buf, j, v, lane)(c);
       }
+      into[v] = at.val();
+      carry[v] = c.val();
     }
   }
 };
@@ -245,7 +310,7 @@ __device__ __forceinline__ void enter_segment(void* ws, size_t N, int g, int w, 
   const int per = (g + S) / S, lo = w * per, hi = lo + per < g + 1 ? lo + per : g + 1;
   Map<DIAG> mine[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) mine[v] = {Val<DIAG>::one(), Val<DIAG>::zero()};
+  for (int v = 0; v < V; ++v) mine[v] = {Wide<DIAG>::one(), Val<DIAG>::zero()};
   for (int i = lo; i < hi; ++i)
 #pragma unroll
     for (int v = 0; v < V; ++v) mine[v] = slot<DIAG>(ws, N, i)[l.c + v].after(mine[v]);
@@ -265,9 +330,14 @@ template <bool DIAG, int V, int S>
 __device__ __forceinline__ void enter_part(void* ws, size_t N, int segments, int g, int w, int lane,
                                            const Lane<DIAG, V>& l, Exchange<DIAG, V, S>& ex, Val<DIAG> (&carry)[V]) {
   enter_segment<DIAG, V, S>(ws, N, g, w, lane, l, ex, carry);
+  Wide<DIAG> c[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) c[v] = Wide<DIAG>::of(carry[v]);
   for (int j = 0; j < w; ++j)
 #pragma unroll
-    for (int v = 0; v < V; ++v) carry[v] = wave_slot<DIAG, S>(ws, N, segments, g, j)[l.c + v](carry[v]);
+    for (int v = 0; v < V; ++v) c[v] = wave_slot<DIAG, S>(ws, N, segments, g, j)[l.c + v](c[v]);
+#pragma unroll
+  for (int v = 0; v < V; ++v) carry[v] = c[v].val();
 }
 
 // After a wave folded its part to `mine`: its map and the segment's.
@@ -283,7 +353,7 @@ __device__ __forceinline__ void leave_part(void* ws, size_t N, int segments, int
     if (w == 0) {
       Map<DIAG> all = mine[v];
 #pragma unroll
-      for (int j = 1; j < S; ++j) all = ex.m[0][j][v][lane].after(all);
+      for (int j = 1; j < S; ++j) all = ex.map(0, j, v, lane).after(all);
       slot<DIAG>(ws, N, g + 1)[l.c + v] = all;
     }
   }
@@ -348,17 +418,22 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u,
 #pragma unroll
       for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
   }
-  VT A[V], B[V];  // the steps so far (SCAN_FOLD) or of this block
+  Wide<DIAG> A[V];  // the steps so far (SCAN_FOLD) or of this block
+  VT B[V];
   bool cut = false;
   auto restart = [&]() {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      A[v] = VT::one();
+      A[v] = Wide<DIAG>::one();
       B[v] = VT::zero();
     }
     cut = false;
   };
   restart();
+  Wide<DIAG> block[V];  // the factor of SCAN_K steps
+  if constexpr (DIAG)
+#pragma unroll
+    for (int v = 0; v < V; ++v) block[v] = power(lam[v]);
   int buf = 0;
   Block<DT, DIAG, V> cur, nxt;
   const int ahead = PARTS ? 0 : w * SCAN_K;
@@ -376,9 +451,15 @@ __global__ __launch_bounds__(64 * S) void scan_kernel(ScanArgs a, const void* u,
             const VT ak = [&] { if constexpr (DIAG) return lam[v]; else return cur.g[k].get(v); }();
             const VT uk = cur.u[k].get(v);
             B[v] = c ? uk : VT::fma(ak, B[v], uk);
-            A[v] = VT::mul(ak, A[v]);
+            if constexpr (!DIAG) take_gate(A[v], ak, k);
           }
           cut |= c;
+        }
+      if constexpr (DIAG)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const Wide<DIAG> steps = power(lam[v], block[v], end - tw);
+          A[v] = MODE == SCAN_FOLD ? Wide<DIAG>::mul(A[v], steps).held() : steps;
         }
     }
     if constexpr (MODE != SCAN_FOLD) {
@@ -452,7 +533,7 @@ struct BackBlock {
 };
 
 template <int DT, bool DIAG, int V, int S, int MODE, bool GRAD>
-__global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void* gate, const uint8_t* done,
+__global__ __launch_bounds__(64 * S, 4) void scan_bwd_kernel(ScanArgs a, const void* gate, const uint8_t* done,
                                                           const float* h0, const void* h, const void* dh,
                                                           const float* dh_last, void* du, void* dgate, float* dh0,
                                                           void* ws, double* dlam_part, int seg) {
@@ -478,12 +559,13 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
 #pragma unroll
       for (int v = 0; v < V; ++v) slot<DIAG>(ws, N, 0)[l.c + v] = Map<DIAG>::constant(carry[v]);
   }
-  VT A[V], B[V];
+  Wide<DIAG> A[V];
+  VT B[V];
   bool cut = false;
   auto restart = [&]() {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      A[v] = VT::one();
+      A[v] = Wide<DIAG>::one();
       B[v] = VT::zero();
     }
     cut = false;
@@ -492,6 +574,10 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
   double sx[V], sy[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) sx[v] = sy[v] = 0.;
+  Wide<DIAG> block[V];  // the factor of SCAN_K steps
+  if constexpr (DIAG)
+#pragma unroll
+    for (int v = 0; v < V; ++v) block[v] = power(lam[v].conj());
   int buf = 0;
   BackBlock<DT, DIAG, V, GRAD> cur, nxt;
   const int ahead = PARTS ? 0 : w * SCAN_K;
@@ -508,9 +594,15 @@ __global__ __launch_bounds__(64 * S) void scan_bwd_kernel(ScanArgs a, const void
           for (int v = 0; v < V; ++v) {
             const VT ak = [&] { if constexpr (DIAG) return lam[v].conj(); else return cur.g[k].get(v); }();
             B[v] = c ? VT::zero() : VT::mul(ak, VT::add(cur.dh[k].get(v), B[v]));
-            A[v] = VT::mul(ak, A[v]);
+            if constexpr (!DIAG) take_gate(A[v], ak, k);
           }
           cut |= c;
+        }
+      if constexpr (DIAG)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const Wide<DIAG> steps = power(lam[v].conj(), block[v], end - rw);
+          A[v] = MODE == SCAN_FOLD ? Wide<DIAG>::mul(A[v], steps).held() : steps;
         }
     }
     if constexpr (MODE != SCAN_FOLD) {

@@ -100,3 +100,86 @@ def test_ppo_rows_of_lowest_logits_only(rows):
     got = R.ppo_loss(**_gpu_args(kw), **HYPER)
     kw["logits"][::3] = 0
     _check_ppo(kw, got, False)
+
+
+# ---- recurrence: gates of any size ----
+
+# segments; 16, 8 and 4 waves of a workgroup, pairs of bfloat16 and single channels; one wave
+GATE_SIZES = [(6400, 1, 1, 16), (900, 33, 2, 210), (900, 16, 3, 211), (300, 28, 2, 512), (300, 150, 2, 256), (48, 500, 2, 256), (32, 3, 1, 5),
+              (16, 3, 1, 5)]
+
+
+def _forward_and_back(s):
+    h, last = R.scan(s.u, s.gate, s.done, s.h0)
+    s.check_forward(h, last)
+    s.check_backward(h, *R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last))
+    return h
+
+
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+@pytest.mark.parametrize("size", [(32768, 1, 1, 16)] + GATE_SIZES)
+def test_scan_of_nothing_is_nothing(kind, size):
+    """Without inputs and state the states are 0, however large the products of the gates (here 1.03 for half of the
+    run, then 0.97, or 1e20 all along)."""
+    T = size[0]
+    for up, down in ((1.03, 0.97), (1e20, 1e20)):
+        s = Scan(kind, "f32", *size, done=None, h0=False, seed=1, radius=up)
+        if kind == "gated":
+            s.gate[:] = up
+            s.gate[T // 2:] = down
+        s.u.zero_()
+        s.dh.zero_()
+        h, last = R.scan(s.u, s.gate)
+        assert (h == 0).all() and (last == 0).all()
+        assert all((g == 0).all() for g in R.scan_backward(s.gate, h, s.dh))
+
+
+@pytest.mark.parametrize("kind", ["gated", "diagonal"])
+def test_scan_inputs_behind_growing_gates(kind):
+    """Inputs in the last 400 steps alone, behind 6000 steps whose gates' product is 1e364 (the gradient: in the
+    first)."""
+    s = Scan(kind, "f32", 6400, 1, 2, 16, done=None, h0=False, seed=2, radius=1.15)
+    s.u[:6000] = 0
+    s.dh[400:] = 0
+    _forward_and_back(s)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("size", GATE_SIZES)
+def test_scan_gates_up_and_down(dt, size):
+    """Gates whose product rises to 1e40 within 8 steps and falls back within the next 8 (values of 1e-30 to 1e10): every
+    state fits float32, the products of the gates do not."""
+    s = Scan("gated", dt, *size, done=0.01, seed=3)
+    t = torch.arange(size[0], device="cuda")
+    # half a period ahead in every second channel
+    phase = (t[:, None, None, None] + 8 * (torch.arange(size[3], device="cuda") % 2)) % 16 < 8
+    s.gate[:] = torch.where(phase, 2.0 ** 17, 2.0 ** -17) * torch.sign(s.gate.float())
+    s.u *= 2.0 ** -100
+    s.h0 *= 2.0 ** -100
+    s.dh *= 2.0 ** -100
+    s.dh_last *= 2.0 ** -100
+    h, last = R.scan(s.u, s.gate, s.done, s.h0)
+    s.check_forward(h, last)
+    h = torch.randn(h.shape, generator=torch.Generator("cuda").manual_seed(5), device="cuda").to(h.dtype)
+    s.h0 = torch.randn_like(s.h0)  # (states of 1: products with the smallest gradients fit float32, too)
+    s.check_backward(h, *R.scan_backward(s.gate, h, s.dh, s.done, s.h0, s.dh_last))
+
+
+@pytest.mark.parametrize("size", [(6400, 1, 1, 16), (6400, 3, 1, 33), (2000, 60, 1, 128)])
+def test_scan_long_rise_and_fall(size):
+    """A product of 1e-60 over 200 steps and back over the next 200: powers of two, so that every state is exact."""
+    T = size[0]
+    s = Scan("gated", "f32", *size, done=None, seed=4)
+    fall = torch.arange(T, device="cuda")[:, None, None, None] % 400 < 200
+    s.gate[:] = torch.where(fall, 0.5, 2.0)
+    s.u.zero_()
+    s.h0[:] = 2.0 ** 100
+    h, last = R.scan(s.u, s.gate, None, s.h0)
+    want, wlast = L.scan(_np(s.u), _np(s.gate), None, _np(s.h0))
+    assert np.array_equal(_np(h), want) and np.array_equal(_np(last), wlast)
+    s.dh.zero_()
+    s.dh_last[:] = 2.0 ** -100
+    du, dgate, dh0 = R.scan_backward(s.gate, torch.zeros_like(h), s.dh, None, torch.zeros_like(s.h0), s.dh_last)
+    wdu, _, wdh0 = L.scan_backward(_np(s.gate), np.zeros(h.shape), _np(s.dh), None, None, _np(s.dh_last))
+    assert np.abs(wdu).max() < FLT_MAX
+    assert np.array_equal(_np(du), wdu) and np.array_equal(_np(dh0), wdh0) and (dgate == 0).all()
