@@ -160,6 +160,15 @@ __device__ __forceinline__ double uniform(double v) {
   return __longlong_as_double((uint64_t)hi << 32 | lo);
 }
 
+__device__ __forceinline__ float uniform(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
+
+// Lane w's value, for every lane.
+__device__ __forceinline__ float of_lane(float v, int w) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), w));
+}
+
 // exp(x): the hardware's 2^t with t = x log2(e) rounded, times
 // 1 + ln(2) (x log2(e) - t); within 3 float32 steps for |x| < 2^100 (results
 // below 2^-126 are 0).
@@ -209,6 +218,16 @@ constexpr float FAR_BELOW = -1e30f, LEAST = -200.f;
 __device__ __forceinline__ float below_top(float x, float top) {
   const float d = x - top;  // (a NaN stays one)
   return x == -INFINITY ? FAR_BELOW : d < LEAST ? LEAST : d;
+}
+
+// v exp(t) / n for a result that fits float32, also where exp(t) or v exp(t)
+// does not: three factors exp(t / 3), in an order in which no product is
+// larger than both v and the result (t beyond 264: infinite for any v).
+__device__ __forceinline__ float times_exp(float v, float t, float inv_n) {
+  const float f = exp32((t > 264.f ? 264.f : t) * (1.f / 3.f));
+  const bool large = fabsf(v) > 1.f;
+  v = (large ? v * inv_n : v) * f;
+  return (large ? v : v * inv_n) * f * f;
 }
 
 // A lane's row in LDS -> registers, and back, by the widest pieces that every
@@ -300,36 +319,32 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
   const bool some = !(sum == 0.f);  // a legal action's term is 1, or NaN
   const float logs = some ? log32(sum) : 0.f, inv = some ? rcp32(sum) : 0.f;
   const float ent = logs - zsum * inv;  // -sum p log p, log p = z - logs
-  float slope = 0.f;                    // d policy / d log p_a
+  float slope = 0.f, adv = 0.f;         // d policy / d log p_a
+  bool rare = false;                    // .. is left to the end
+  const double lo64 = uniform(1. - (double)p.clip), hi64 = uniform(1. + (double)p.clip);
+  const float lo = uniform((float)lo64), hi = uniform((float)hi64);
   if (!(xa == -INFINITY)) {
-    const float adv = (float)(((double)adv_in - nm.mean) * nm.rstd);
-    const float lo = (float)(1. - (double)p.clip), hi = (float)(1. + (double)p.clip);
+    adv = (float)(((double)adv_in - nm.mean) * nm.rstd);
     const double diff64 = (double)xa - top - logs - old;  // (of float32 it may pass the range)
     const float diff = (float)diff64, ratio = exp32(diff > 200.f ? 200.f : diff < -200.f ? -200.f : diff);
-    bool below = ratio < lo, above = ratio > hi;
-    // near a border the float32 ratio does not say on which side it lies (the borders' own rounding is within tol)
-    const float tol = 1e-6f * (16.f + fabsf(xa) + fabsf(top) + fabsf(old)) * ratio;
-    if (fabsf(ratio - lo) <= tol || fabsf(ratio - hi) <= tol) {
-      // (xa less the log of the sum, less old) against log(1 -+ clip), without logarithms
-      double s64 = 0.;
-#pragma unroll 1
-      for (int i = 0; i < NA; ++i) s64 += x[i] == -INFINITY ? 0. : exp64((double)x[i] - (double)top);
-      const double e64 = exp64((double)xa - (double)top - (double)old);
-      below = e64 < (1. - (double)p.clip) * s64;
-      above = e64 > (1. + (double)p.clip) * s64;
-    }
-    const float clipped = above ? hi : below ? lo : ratio;
+    const bool below = ratio < lo, above = ratio > hi;
     // the smaller surrogate is the plain one unless the ratio has left the range on the advantage's side
     const bool plain = adv > 0.f ? !above : adv < 0.f ? !below : true;
-    st[1] -= (double)((plain ? ratio : clipped) * adv);
-    slope = plain ? -adv * ratio : 0.f;
-    st[4] += (double)ratio - 1. - diff64;
-    st[5] += below || above ? 1. : 0.;
+    // near a border the float32 ratio does not say on which side it lies (the borders' own rounding is within tol), and
+    // it may be infinite or make such a product where float64's does not
+    const float tol = 1e-6f * (16.f + fabsf(xa) + fabsf(top) + fabsf(old)) * ratio, product = ratio * adv;
+    rare = fabsf(ratio - lo) <= tol || fabsf(ratio - hi) <= tol || !(fabsf(product) <= 1e30f);
+    if (!rare) {
+      st[1] -= (double)(plain ? product : (above ? hi : below ? lo : ratio) * adv);
+      slope = plain ? -product : 0.f;
+      st[4] += (double)ratio - 1. - diff64;
+      st[5] += below || above ? 1. : 0.;
+    }
   }
   if (counted && some) st[3] += (double)ent;
   double dv = 0.;
   if (counted) {
-    const double err = (double)value - ret, off = (double)value - value_old, vc = p.value_clip;
+    const double err = (double)value - ret, off = (double)value - value_old, vc = uniform((double)p.value_clip);
     double loss = 0.5 * err * err;
     dv = err;
     if (vc > 0. && fabs(off) > vc) {
@@ -341,16 +356,44 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     }
     st[2] += loss;
   }
-  if (real) (p.dvalue + r0)[r] = (float)((double)p.value_coef * dv * nm.inv_n);
-  // slope (onehot - p) + c p (log p + H), over n
-  const float inv_n = (float)nm.inv_n, c = p.entropy_coef, shift = ent - logs, back = slope * inv_n;
+  if (real) (p.dvalue + r0)[r] = (float)(uniform((double)p.value_coef * nm.inv_n) * dv);
+  // slope (onehot - p) + c p (log p + H), over n; where p is 0 so is its part of both
+  const float inv_n = uniform((float)nm.inv_n), c = uniform(p.entropy_coef * inv_n), shift = ent - logs;
+  const float back = slope * inv_n;
   const bool any = counted && some;
 #pragma unroll
   for (int i = 0; i < NA; ++i) {
-    const float d = fmaf(e[i] * inv, (c * (z[i] + shift) - slope) * inv_n, i == act ? back : 0.f);
+    const float q = e[i] * inv, d = fmaf(c, q * (z[i] + shift), fmaf(-back, q, i == act ? back : 0.f));
     z[i] = any && !(z[i] == FAR_BELOW) ? d : 0.f;
   }
-  row_out<NA>(x, z);
+  if (!rare) row_out<NA>(x, z);
+  // the rare rows, each by the whole wave (a lane to an action), in float64
+  for (uint64_t left = __ballot(rare); left != 0; left &= left - 1) {
+    const int w = __ffsll((unsigned long long)left) - 1, wact = __builtin_amdgcn_readlane(act, w);
+    const float wtop = of_lane(top, w), wlogs = of_lane(logs, w), winv = of_lane(inv, w), wadv = of_lane(adv, w);
+    const double arg = (double)of_lane(xa, w) - (double)wtop - (double)of_lane(old, w), diff64 = arg - (double)wlogs;
+    float* row = s + w * LD;
+    const float xi = lane < NA ? row[lane] : -INFINITY;
+    // (xa less the log of the sum, less old) against log(1 -+ clip), without logarithms: lane 32 (no action's) has the
+    // exponential of the first part.  (e^600 times any advantage fits float64, and is infinite in float32 as it has to be)
+    const double mine = exp64(lane == 32 ? (arg > 600. ? 600. : arg) : (double)xi - (double)wtop);
+    double s64 = xi == -INFINITY ? 0. : mine;
+    for (int d = 32; d > 0; d >>= 1) s64 += __shfl_xor(s64, d, 64);
+    const double e64 = __shfl(mine, 32, 64), ratio = e64 / s64;
+    const bool below = e64 < lo64 * s64, above = e64 > hi64 * s64;
+    const bool plain = wadv > 0.f ? !above : wadv < 0.f ? !below : true;
+    if (lane == w) {
+      st[1] -= (plain ? ratio : above ? (double)hi : below ? (double)lo : ratio) * (double)wadv;
+      st[4] += ratio - 1. - diff64;
+      st[5] += below || above ? 1. : 0.;
+    }
+    // slope (onehot - p) with ratio and p by their logarithms
+    const float zi = below_top(xi, wtop), q = exp32(zi) * winv, by = plain ? wadv : 0.f, diff = (float)diff64;
+    const bool me = lane == wact;
+    const float d = times_exp(me ? -by * (1.f - q) : by, me ? diff : diff + (zi - wlogs), inv_n);
+    const float wshift = of_lane(shift, w);
+    if (lane < NA) row[lane] = zi == FAR_BELOW ? 0.f : fmaf(c, q * (zi + wshift), zi == LEAST && !me ? 0.f : d);
+  }
   wave_lds_sync();
   float* out = p.dlogits + r0 * NA;
   if (live == 64 && (reinterpret_cast<uintptr_t>(p.dlogits) & 15) == 0) {

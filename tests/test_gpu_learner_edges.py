@@ -183,3 +183,76 @@ def test_scan_long_rise_and_fall(size):
     wdu, _, wdh0 = L.scan_backward(_np(s.gate), np.zeros(h.shape), _np(s.dh), None, None, _np(s.dh_last))
     assert np.abs(wdu).max() < FLT_MAX
     assert np.array_equal(_np(du), wdu) and np.array_equal(_np(dh0), wdh0) and (dgate == 0).all()
+
+
+# ---- PPO: ratios and advantages beyond float32 ----
+
+
+def _check_wide(kw, got, hyper=HYPER):
+    """Against the oracle where outputs may pass float32's range (then: infinite, of that sign).  A gradient's policy part
+    is slope (onehot - p): the slope is off by t + 4 u of itself, p by t (t of test_gpu_learner.py), so together at most
+    (2 t + 16 u) |slope| (onehot + p), and what float32 cannot hold (below 2^-126) is lost."""
+    h, f = _hyper64(hyper), _f64(kw)
+    wdx, wdv, wst = L.ppo_loss(**f, **h)
+    rows, na = kw["logits"].shape
+    x = np.maximum(f["logits"], -150.0)
+    p = np.exp(x - x.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    a = np.clip(kw["actions"], 0, na - 1)
+    acts = (kw["actions"] == a).astype(float)
+    t = U32 * (16 + 4 * np.abs(x).max(1) + 2 * np.abs(f["logp_old"]))
+    slope = np.abs(f["adv"]) * np.exp(np.log(p[np.arange(rows), a]) - f["logp_old"]) * acts
+    tol = ((2 * t + 16 * U32) * slope)[:, None] * (p + (np.arange(na) == a[:, None]))
+    tol += ((t + 16 * U32) * h["entropy_coef"])[:, None] * (np.abs(np.log(p)) * p + 4)
+    for name, g, want, tol in (("dlogits", _np(got[0]), wdx, tol / rows + 2.0 ** -126),
+                               ("dvalue", _np(got[1]), wdv, 4 * U32 * np.abs(wdv)),
+                               ("stats", _np(got[2]), wst, (2 * t.max() + 16 * U32) * (np.abs(wst) + np.abs(wst[1:4]).sum()) +
+                                t.max() * (np.arange(6) != 5))):
+        assert not np.isnan(g).any(), (name, np.argwhere(np.isnan(g))[:4].tolist())
+        over = np.abs(want) - tol > FLT_MAX
+        assert (g[over] == np.sign(want[over]) * np.inf).all(), name
+        fine = np.abs(want) + tol < FLT_MAX
+        _close(g[fine], want[fine], tol[fine], name)
+
+
+@ROUTES
+@pytest.mark.parametrize("lo,hi,scale", [(60, 85, 1e-6), (85, 95, 1e-12), (89, 200, 1e-3), (1, 3, 3e38)])
+def test_ppo_ratios_beyond_float32(rows, lo, hi, scale):
+    """Log ratios of lo to hi (float32's exp ends at 88.7), advantages of both signs and 0; some probabilities are tiny,
+    some 0.  Gradients that fit float32 are right, also where the ratio or the slope does not fit."""
+    rng = np.random.default_rng(rows + hi)
+    kw = _ppo(rows, 6, seed=rows + 8, spread=3.0)
+    x = kw["logits"]
+    x[rng.random((rows, 6)) < 0.2] = -60
+    x[rng.random((rows, 6)) < 0.2] = LOWEST
+    x[:, 2] = rng.standard_normal(rows)
+    kw["actions"] = np.where(rng.random(rows) < 0.7, 2, 3).astype(np.int32)
+    kw["actions"][x[np.arange(rows), kw["actions"]] < -50] = 2
+    x64 = np.maximum(x.astype(np.float64), -150)
+    lp = x64 - np.log(np.exp(x64).sum(1, keepdims=True))
+    kw["logp_old"] = (lp[np.arange(rows), kw["actions"]] - rng.uniform(lo, hi, rows)).astype(np.float32)
+    kw["adv"] = (scale * rng.uniform(-1, 1, rows) * (rng.random(rows) < 0.8)).astype(np.float32)
+    _check_wide(kw, R.ppo_loss(**_gpu_args(kw), **HYPER))
+
+
+@ROUTES
+def test_ppo_ratios_beyond_float64(rows):
+    """Log ratios of 1000: an action of probability 0 has gradient 0, the taken one's is infinite, nothing is NaN."""
+    kw = _ppo(rows, 6, seed=rows + 10)
+    kw["actions"][:] = 1
+    kw["logits"][:, 4] = LOWEST
+    kw["logp_old"][:] = -1000
+    kw["adv"] = np.where(np.arange(rows) % 3 == 0, -1.0, np.where(np.arange(rows) % 3 == 1, 0.0, 1.0)).astype(np.float32)
+    dx, dv, st = (_np(t) for t in R.ppo_loss(**_gpu_args(kw), **HYPER))
+    assert not np.isnan(dx).any() and (dx[:, 4] == 0).all()
+    assert np.isposinf(dx[::3, 1]).all() and np.isfinite(dx[1::3]).all() and np.isfinite(dx[2::3]).all()
+    assert np.isposinf(st[[0, 1, 4]]).all() and np.isfinite(st[[2, 3, 5]]).all() and np.isfinite(dv).all()
+
+
+@ROUTES
+def test_ppo_entropy_coefficient_of_any_size(rows):
+    """Probabilities of 0 add no gradient, however large the coefficient is."""
+    kw, low = _with_low(rows, rows + 12, taken=False)
+    kw["logits"][low] = LOWEST
+    dx, _, _ = R.ppo_loss(**_gpu_args(kw), **dict(HYPER, entropy_coef=1e37))
+    assert (dx[torch.from_numpy(low).cuda()] == 0).all() and not bool(torch.isnan(dx).any())
