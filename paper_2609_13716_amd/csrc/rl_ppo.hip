@@ -29,9 +29,21 @@ inline bool ppo_small(int64_t R, int na) { return R * (na + 8) <= 40 * 1024; }
 constexpr int PPO_ADV_B = 64, PPO_ROW_B = 512;  // workgroups, at most (their partial sums go to the workspace)
 constexpr int PPO_STATS = 6;
 
+// Counted rows, and the sum and sum of squares of their advantages less `from`,
+// one of them: so a mean far from 0 costs no digits of the variance.
+struct AdvSum {
+  double n, sum, sq, from;
+  __device__ void add(bool in, float adv) {
+    if (in && n == 0.) from = (double)adv;
+    const double a = in ? (double)adv - from : 0.;  // (a padded row's value is dropped)
+    n += in ? 1. : 0.;
+    sum += a;
+    sq += a * a;
+  }
+};
+
 struct PpoPart {  // workspace
-  double shift;              // what the advantages' sums are taken from
-  double adv[PPO_ADV_B][3];  // rows counted, sum and sum of squares of their advantages
+  AdvSum adv[PPO_ADV_B];
   double stat[PPO_ROW_B][PPO_STATS];
 };
 
@@ -44,20 +56,28 @@ __device__ __forceinline__ void wave_sum(double (&v)[N]) {
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d, 64);
 }
 
-// The same over a workgroup of at most 16 waves, for every thread.
-template <int N>
-__device__ __forceinline__ void block_sum(double (&v)[N], double (*s)[N]) {
-  wave_sum<N>(v);
+// The lanes' sums put together, for every lane: all taken from the value of the
+// first lane that has one.
+__device__ __forceinline__ AdvSum wave_sum(const AdvSum& mine) {
+  const uint64_t some = __ballot(mine.n > 0.);
+  AdvSum r{};
+  if (some) r.from = __shfl(mine.from, __ffsll((unsigned long long)some) - 1, 64);
+  const double d = mine.from - r.from;
+  double v[3] = {mine.n, mine.n > 0. ? mine.sum + mine.n * d : 0., mine.n > 0. ? mine.sq + d * (2. * mine.sum + mine.n * d) : 0.};
+  wave_sum<3>(v);
+  r.n = v[0];
+  r.sum = v[1];
+  r.sq = v[2];
+  return r;
+}
+
+// The same over a workgroup (s: one for each wave), for every thread.
+__device__ __forceinline__ AdvSum block_sum(const AdvSum& mine, AdvSum* s) {
+  const AdvSum v = wave_sum(mine);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-  if (lane == 0)
-    for (int i = 0; i < N; ++i) s[w][i] = v[i];
+  if (lane == 0) s[w] = v;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = (lane & 15) < nw ? s[lane & 15][i] : 0.;
-#pragma unroll 1
-  for (int d = 8; d > 0; d >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], d, 64);
+  return wave_sum(lane < nw ? s[lane] : AdvSum{});
 }
 
 // Sums of the statistics over a workgroup: v[i] into thread i < PPO_STATS's
@@ -83,41 +103,24 @@ __device__ __forceinline__ double stats_sum(const double (&v)[PPO_STATS], double
   return t;
 }
 
-// An advantage that the sums are taken from, so that a mean far from 0 costs
-// no digits of the variance: the first counted one of 64 rows spread evenly.
-__device__ __forceinline__ double adv_shift(const PpoArgs& p) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r = lane * p.R / 64;
-  const float a = p.adv[r];
-  const uint64_t some = __ballot((!p.mask || p.mask[r]) && fabsf(a) < INFINITY);
-  return some ? (double)__shfl(a, __ffsll((unsigned long long)some) - 1, 64) : 0.;
-}
-
-// Counted rows, and the sum and sum of squares of their advantages less `shift`.
-__device__ __forceinline__ void adv_sums(const PpoArgs& p, double shift, int64_t first, int64_t step, double (&v)[3]) {
+// A thread's part of the rows.
+__device__ __forceinline__ AdvSum adv_sums(const PpoArgs& p, int64_t first, int64_t step) {
+  AdvSum v{};
 #pragma unroll 8
   for (int64_t r = first; r < p.R; r += step) {
     const uint8_t in = p.mask ? p.mask[r] : 1;
-    const float read = p.adv[r];  // (before the mask is known; a padded row's value is dropped)
-    const double a = in ? (double)read - shift : 0.;
-    v[0] += in ? 1. : 0.;
-    v[1] += a;
-    v[2] += a * a;
+    const float read = p.adv[r];  // (before the mask is known)
+    v.add(in, read);
   }
+  return v;
 }
 
 // The same, four neighbouring rows at a time, ADV_U times that in flight;
 // false (and nothing done) where the arrays are not aligned to that.
 constexpr int ADV_U = 4;
-__device__ __forceinline__ bool adv_sums4(const PpoArgs& p, double shift, int64_t first, int64_t step, double (&v)[3]) {
+__device__ __forceinline__ bool adv_sums4(const PpoArgs& p, int64_t first, int64_t step, AdvSum& v) {
   if ((reinterpret_cast<uintptr_t>(p.adv) & 15) | (reinterpret_cast<uintptr_t>(p.mask) & 3)) return false;
   const int64_t fours = p.R / 4;
-  auto add = [&](bool in, float read) {
-    const double a = in ? (double)read - shift : 0.;
-    v[0] += in ? 1. : 0.;
-    v[1] += a;
-    v[2] += a * a;
-  };
   for (int64_t r = first; r < fours; r += ADV_U * step) {
     f32x4 a[ADV_U];
     uint32_t in[ADV_U];
@@ -131,23 +134,22 @@ __device__ __forceinline__ bool adv_sums4(const PpoArgs& p, double shift, int64_
     for (int q = 0; q < ADV_U; ++q) {
       if (r + q * step >= fours) in[q] = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) add(in[q] >> 8 * k & 255, a[q][k]);
+      for (int k = 0; k < 4; ++k) v.add(in[q] >> 8 * k & 255, a[q][k]);
     }
   }
   const int64_t rest = 4 * fours + first;
-  if (rest < p.R) add(!p.mask || p.mask[rest], p.adv[rest]);
+  if (rest < p.R) v.add(!p.mask || p.mask[rest], p.adv[rest]);
   return true;
 }
 
 struct PpoNorm {
   double inv_n, mean, rstd;
 };
-// From the counted rows' number, sum and sum of squares.
-__device__ __forceinline__ PpoNorm ppo_norm(const PpoArgs& p, double shift, const double (&v)[3]) {
-  PpoNorm r{1. / (v[0] > 0. ? v[0] : 1.), 0., 1.};
+__device__ __forceinline__ PpoNorm ppo_norm(const PpoArgs& p, const AdvSum& v) {
+  PpoNorm r{1. / (v.n > 0. ? v.n : 1.), 0., 1.};
   if (p.normalize) {
-    const double off = v[1] * r.inv_n, var = v[2] * r.inv_n - off * off;
-    r.mean = shift + off;
+    const double off = v.sum * r.inv_n, var = v.sq * r.inv_n - off * off;
+    r.mean = v.from + off;
     r.rstd = 1. / (sqrt(var < 0. ? 0. : var) + 1e-8);  // (a NaN stays one)
   }
   return r;
@@ -417,15 +419,12 @@ __device__ __forceinline__ void ppo_means(const PpoArgs& p, const double (&v)[PP
 }
 
 __global__ __launch_bounds__(PPO_SUM_NT) void ppo_adv_kernel(PpoArgs p, PpoPart* part) {
-  __shared__ double s[16][3];
-  double v[3] = {0., 0., 0.};
-  const double shift = p.normalize ? adv_shift(p) : 0.;
-  if (blockIdx.x == 0 && threadIdx.x == 0) part->shift = shift;
+  __shared__ AdvSum s[PPO_SUM_NT / 64];
   const int64_t first = (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, step = (int64_t)gridDim.x * PPO_SUM_NT;
-  if (!adv_sums4(p, shift, first, step, v)) adv_sums(p, shift, first, step, v);
-  block_sum<3>(v, s);
-  if (threadIdx.x == 0)
-    for (int i = 0; i < 3; ++i) part->adv[blockIdx.x][i] = v[i];
+  AdvSum v{};
+  if (!adv_sums4(p, first, step, v)) v = adv_sums(p, first, step);
+  v = block_sum(v, s);
+  if (threadIdx.x == 0) part->adv[blockIdx.x] = v;
 }
 
 // LDS bytes of a wave: its rows, or its statistics at the end.
@@ -444,12 +443,8 @@ __global__ __launch_bounds__(PPO_NT, NA <= 20 ? 4 : 1) void ppo_rows_kernel(PpoA
   __shared__ double s_stat[16][PPO_STATS];
   PpoNorm nm{1. / (double)p.R, 0., 1.};
   if (adv_blocks) {  // every wave for itself: one partial sum per lane
-    double v[3] = {0., 0., 0.};
     const int b = threadIdx.x & 63;  // (PPO_ADV_B <= 64)
-    if (b < adv_blocks)
-      for (int i = 0; i < 3; ++i) v[i] = part->adv[b][i];
-    wave_sum<3>(v);
-    nm = ppo_norm(p, part->shift, v);
+    nm = ppo_norm(p, wave_sum(b < adv_blocks ? part->adv[b] : AdvSum{}));
     nm = {uniform(nm.inv_n), uniform(nm.mean), uniform(nm.rstd)};
   }
   double st[PPO_STATS] = {0., 0., 0., 0., 0., 0.};
@@ -470,7 +465,7 @@ __global__ __launch_bounds__(STATS_NT) void ppo_stats_kernel(PpoArgs p, const Pp
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   double v = 0.;
   if (w == 0)
-    for (int b = lane; b < adv_blocks; b += 64) v += part->adv[b][0];
+    for (int b = lane; b < adv_blocks; b += 64) v += part->adv[b].n;
   else
     for (int b = lane; b < blocks; b += 64) v += part->stat[b][w];
 #pragma unroll 1
@@ -488,12 +483,9 @@ __global__ __launch_bounds__(STATS_NT) void ppo_stats_kernel(PpoArgs p, const Pp
 template <int NA>
 __global__ __launch_bounds__(PPO_NT) void ppo_small_kernel(PpoArgs p) {
   extern __shared__ double s_dyn[];
-  __shared__ double s_adv[16][3], s_stat[16][PPO_STATS], s_all[PPO_STATS];
-  double v[3] = {0., 0., 0.};
-  const double shift = p.normalize ? adv_shift(p) : 0.;
-  adv_sums(p, shift, threadIdx.x, blockDim.x, v);
-  block_sum<3>(v, s_adv);
-  const PpoNorm nm = ppo_norm(p, shift, v);
+  __shared__ AdvSum s_adv[PPO_NT / 64];
+  __shared__ double s_stat[16][PPO_STATS], s_all[PPO_STATS];
+  const PpoNorm nm = ppo_norm(p, block_sum(adv_sums(p, threadIdx.x, blockDim.x), s_adv));
   double st[PPO_STATS] = {0., 0., 0., 0., 0., 0.};
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   char* mine = reinterpret_cast<char*>(s_dyn) + w * ppo_wave_bytes(NA);

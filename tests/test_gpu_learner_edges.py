@@ -256,3 +256,19 @@ def test_ppo_entropy_coefficient_of_any_size(rows):
     kw["logits"][low] = LOWEST
     dx, _, _ = R.ppo_loss(**_gpu_args(kw), **dict(HYPER, entropy_coef=1e37))
     assert (dx[torch.from_numpy(low).cuda()] == 0).all() and not bool(torch.isnan(dx).any())
+
+
+# ---- PPO: advantages ----
+
+
+@pytest.mark.parametrize("rows", [2048, 2900, 32768, 65536])
+@pytest.mark.parametrize("mean,scale", [(3000.0, 0.01), (-2e6, 1.0), (7.0, 0.0)])
+def test_ppo_advantages_under_any_mask(rows, mean, scale):
+    """Masks with the period of agents, and ones that leave a few rows anywhere: the mean may lie far from 0."""
+    for pick in (lambda r: r % 2 == 1, lambda r: r % 4 == 2, lambda r: r >= rows - 7, lambda r: r == rows // 2 + 3,
+                 lambda r: (r > 700) & (r < 760)):
+        kw = _ppo(rows, 6, seed=14)
+        kw["adv"] = (mean + scale * np.random.default_rng(15).standard_normal(rows)).astype(np.float32)
+        kw["mask"] = pick(np.arange(rows)).astype(np.uint8)
+        kw["adv"][kw["mask"] == 0] = np.nan
+        _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True), True)
