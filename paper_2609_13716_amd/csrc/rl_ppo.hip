@@ -115,20 +115,30 @@ __device__ __forceinline__ AdvSum adv_sums(const PpoArgs& p, int64_t first, int6
   return v;
 }
 
-// The same, four neighbouring rows at a time, ADV_U times that in flight;
-// false (and nothing done) where the arrays are not aligned to that.
+// The same, four neighbouring rows at a time, ADV_U times that in flight; the
+// same rows in the same order where they are not aligned to that.
 constexpr int ADV_U = 4;
-__device__ __forceinline__ bool adv_sums4(const PpoArgs& p, int64_t first, int64_t step, AdvSum& v) {
-  if ((reinterpret_cast<uintptr_t>(p.adv) & 15) | (reinterpret_cast<uintptr_t>(p.mask) & 3)) return false;
+__device__ __forceinline__ AdvSum adv_sums4(const PpoArgs& p, int64_t first, int64_t step) {
+  const bool whole = ((reinterpret_cast<uintptr_t>(p.adv) & 15) | (reinterpret_cast<uintptr_t>(p.mask) & 3)) == 0;
   const int64_t fours = p.R / 4;
+  AdvSum v{};
   for (int64_t r = first; r < fours; r += ADV_U * step) {
     f32x4 a[ADV_U];
     uint32_t in[ADV_U];
 #pragma unroll
     for (int q = 0; q < ADV_U; ++q) {
       const int64_t at = r + q * step < fours ? r + q * step : r;  // (past the last ones: read again, not counted)
-      a[q] = reinterpret_cast<const f32x4*>(p.adv)[at];
-      in[q] = p.mask ? reinterpret_cast<const uint32_t*>(p.mask)[at] : 0x01010101u;
+      if (whole) {
+        a[q] = reinterpret_cast<const f32x4*>(p.adv)[at];
+        in[q] = p.mask ? reinterpret_cast<const uint32_t*>(p.mask)[at] : 0x01010101u;
+      } else {
+        in[q] = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          a[q][k] = p.adv[4 * at + k];
+          in[q] |= (p.mask ? (uint32_t)p.mask[4 * at + k] : 1u) << 8 * k;
+        }
+      }
     }
 #pragma unroll
     for (int q = 0; q < ADV_U; ++q) {
@@ -139,7 +149,7 @@ __device__ __forceinline__ bool adv_sums4(const PpoArgs& p, int64_t first, int64
   }
   const int64_t rest = 4 * fours + first;
   if (rest < p.R) v.add(!p.mask || p.mask[rest], p.adv[rest]);
-  return true;
+  return v;
 }
 
 struct PpoNorm {
@@ -421,9 +431,7 @@ __device__ __forceinline__ void ppo_means(const PpoArgs& p, const double (&v)[PP
 __global__ __launch_bounds__(PPO_SUM_NT) void ppo_adv_kernel(PpoArgs p, PpoPart* part) {
   __shared__ AdvSum s[PPO_SUM_NT / 64];
   const int64_t first = (int64_t)blockIdx.x * PPO_SUM_NT + threadIdx.x, step = (int64_t)gridDim.x * PPO_SUM_NT;
-  AdvSum v{};
-  if (!adv_sums4(p, first, step, v)) v = adv_sums(p, first, step);
-  v = block_sum(v, s);
+  const AdvSum v = block_sum(adv_sums4(p, first, step), s);
   if (threadIdx.x == 0) part->adv[blockIdx.x] = v;
 }
 

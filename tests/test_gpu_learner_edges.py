@@ -272,3 +272,30 @@ def test_ppo_advantages_under_any_mask(rows, mean, scale):
         kw["mask"] = pick(np.arange(rows)).astype(np.uint8)
         kw["adv"][kw["mask"] == 0] = np.nan
         _check_ppo(kw, R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True), True)
+
+
+@pytest.mark.parametrize("rows", [300, 30000, 30001])
+def test_ppo_rows_at_any_alignment(rows):
+    """Equal values give equal bits wherever they lie: sums are taken in an order that depends on the sizes only."""
+    kw = _ppo(rows, 6, seed=16, masked=True, padded=True)
+    want = R.ppo_loss(**_gpu_args(kw), **HYPER, normalize=True)
+    for off in (1, 2, 3, 4):
+        got = R.ppo_loss(**_gpu_args(kw, off=off), **HYPER, normalize=True)
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), off
+
+
+@pytest.mark.parametrize("rows", [3000, 30001])
+def test_ppo_sums_in_one_order(rows):
+    """Advantages that cancel but for what their sum rounds off, so that any other order of it shows: the same bits
+    wherever they lie."""
+    rng = np.random.default_rng(21)
+    kw = _ppo(rows, 6, seed=22)
+    half = (rng.standard_normal(rows // 2) * 10.0 ** rng.uniform(-10, 10, rows // 2)).astype(np.float32)
+    kw["adv"] = np.concatenate([half, -half, np.zeros(rows % 2, np.float32)])[rng.permutation(rows)]
+    for mask in (None, np.ones(rows, np.uint8)):
+        kw["mask"] = mask
+        hyper = dict(HYPER, entropy_coef=0.0)
+        want = R.ppo_loss(**_gpu_args(kw), **hyper, normalize=True)
+        for off in (1, 2, 3, 4):
+            got = R.ppo_loss(**_gpu_args(kw, off=off), **hyper, normalize=True)
+            assert all(torch.equal(x, y) for x, y in zip(got, want)), off
