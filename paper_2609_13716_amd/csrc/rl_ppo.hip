@@ -62,8 +62,8 @@ __device__ __forceinline__ AdvSum wave_sum(const AdvSum& mine) {
   const uint64_t some = __ballot(mine.n > 0.);
   AdvSum r{};
   if (some) r.from = __shfl(mine.from, __ffsll((unsigned long long)some) - 1, 64);
-  const double d = mine.from - r.from;
-  double v[3] = {mine.n, mine.n > 0. ? mine.sum + mine.n * d : 0., mine.n > 0. ? mine.sq + d * (2. * mine.sum + mine.n * d) : 0.};
+  const double d = mine.n > 0. ? mine.from - r.from : 0.;
+  double v[3] = {mine.n, mine.sum + mine.n * d, mine.sq + d * (2. * mine.sum + mine.n * d)};
   wave_sum<3>(v);
   r.n = v[0];
   r.sum = v[1];
@@ -199,6 +199,15 @@ __device__ __forceinline__ float log32(float x) {
 __device__ __forceinline__ float rcp32(float x) {
   const float r = __builtin_amdgcn_rcpf(x);
   return fmaf(fmaf(-x, r, 1.f), r, r);
+}
+
+// r - 1 - d for r = exp(d), whose rounding it would be near d = 0: there the sum
+// of d^k / k! from 2 to 7 (for |d| < 1/4 the next term is 2e-8 of it).
+__device__ __forceinline__ double kl_term(double r, double d) {
+  const float x = (float)d;
+  const float s3 = fmaf(x, fmaf(x, fmaf(x, 1.f / 5040.f, 1.f / 720.f), 1.f / 120.f), 1.f / 24.f);
+  const float s = fmaf(x, fmaf(x, s3, 1.f / 6.f), 0.5f);
+  return fabsf(x) < 0.25f ? (double)(x * x * s) : r - 1. - d;
 }
 
 // exp(x) in float64, to 1e-13: 2^k times the Taylor sum of exp(r) to r^12 / 12!
@@ -349,7 +358,7 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     if (!rare) {
       st[1] -= (double)(plain ? product : (above ? hi : below ? lo : ratio) * adv);
       slope = plain ? -product : 0.f;
-      st[4] += (double)ratio - 1. - diff64;
+      st[4] += kl_term((double)ratio, diff64);
       st[5] += below || above ? 1. : 0.;
     }
   }
@@ -387,7 +396,7 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     float* row = s + w * LD;
     const float xi = lane < NA ? row[lane] : -INFINITY;
     // (xa less the log of the sum, less old) against log(1 -+ clip), without logarithms: lane 32 (no action's) has the
-    // exponential of the first part.  (e^600 times any advantage fits float64, and is infinite in float32 as it has to be)
+    // exponential of all but the sum (e^600 times any advantage fits float64, and is infinite in float32 as it should)
     const double mine = exp64(lane == 32 ? (arg > 600. ? 600. : arg) : (double)xi - (double)wtop);
     double s64 = xi == -INFINITY ? 0. : mine;
     for (int d = 32; d > 0; d >>= 1) s64 += __shfl_xor(s64, d, 64);
@@ -396,7 +405,7 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     const bool plain = wadv > 0.f ? !above : wadv < 0.f ? !below : true;
     if (lane == w) {
       st[1] -= (plain ? ratio : above ? (double)hi : below ? (double)lo : ratio) * (double)wadv;
-      st[4] += ratio - 1. - diff64;
+      st[4] += kl_term(ratio, diff64);
       st[5] += below || above ? 1. : 0.;
     }
     // slope (onehot - p) with ratio and p by their logarithms

@@ -299,3 +299,28 @@ def test_ppo_sums_in_one_order(rows):
         for off in (1, 2, 3, 4):
             got = R.ppo_loss(**_gpu_args(kw, off=off), **hyper, normalize=True)
             assert all(torch.equal(x, y) for x, y in zip(got, want)), off
+
+
+# ---- PPO: small KL estimates ----
+
+
+@pytest.mark.parametrize("rows", [500, 30000])
+@pytest.mark.parametrize("delta", [0.0, 1e-4, 1e-3, 0.1, 0.3])
+def test_ppo_kl_of_a_close_policy(rows, delta):
+    """r - 1 - log r near r = 1 is about (log r)^2 / 2 and never negative.  log r is off by t (test_gpu_learner.py), so a
+    row's term by |r - 1| t + r t^2, and by 8 u of itself."""
+    rng = np.random.default_rng(rows)
+    kw = _ppo(rows, 6, seed=17)
+    kw["actions"] = np.clip(kw["actions"], 0, 5).astype(np.int32)
+    x = kw["logits"].astype(np.float64)
+    lp = (x - np.log(np.exp(x).sum(1, keepdims=True)))[np.arange(rows), kw["actions"]]
+    kw["logp_old"] = (lp + delta * rng.uniform(-1, 1, rows)).astype(np.float32)
+    got = R.ppo_loss(**_gpu_args(kw), **HYPER)
+    old = kw["logp_old"].astype(np.float64)
+    r = np.exp(lp - old)
+    t = U32 * (16 + 4 * np.abs(x).max(1) + 2 * np.abs(old))
+    want = L.ppo_loss(**_f64(kw), **_hyper64())[2][4]
+    tol = (np.abs(r - 1) * t + r * t * t).mean() + 8 * U32 * want
+    kl = float(got[2][4])
+    assert kl >= 0 and abs(kl - want) <= tol, (kl, want, tol)
+    _check_ppo(kw, got, False)
