@@ -201,13 +201,13 @@ bool overlap(const Span& a, const Span& b) {
   return x < y + b.bytes && y < x + a.bytes;
 }
 
-// Whether an output overlaps an input or another output; (pin, pout) is the
-// one pair that may be the same array.
+// Whether an output overlaps an input or another output; in[pi] and out[po]
+// are the one pair that may be the same array (-1: there is none).
 template <size_t NI, size_t NO>
-bool aliased(const Span (&in)[NI], const Span (&out)[NO], const void* pin = nullptr, const void* pout = nullptr) {
+bool aliased(const Span (&in)[NI], const Span (&out)[NO], int pi = -1, int po = -1) {
   for (size_t o = 0; o < NO; ++o) {
     for (size_t i = 0; i < NI; ++i) {
-      const bool allowed = pout && pin == pout && out[o].p == pout && in[i].p == pin;
+      const bool allowed = (int)i == pi && (int)o == po && in[i].p == out[o].p;
       if (!allowed && overlap(in[i], out[o])) return true;
     }
     for (size_t q = 0; q < o; ++q)
@@ -604,7 +604,7 @@ rl_status rl_scan(const rl_scan_config* cfg, const void* u, const void* gate, co
   const ScanBytes b = scan_bytes(a);
   const Span in[] = {{u, b.values}, {gate, b.gate}, {done, b.done}, {h0, b.state}};
   const Span out[] = {{h, b.values}, {h_last, b.state}, {workspace, workspace_bytes}};
-  if (aliased(in, out, h0, h_last)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (aliased(in, out, 3, 1)) return fail(RL_EINVAL, "an output overlaps another array");
   if (!scan_aligned(a, {u, h}, {h0, h_last}, gate)) return fail(RL_EINVAL, "an array is not aligned to its elements");
   const size_t need = rl::scan_workspace_bytes(a, false);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
@@ -623,7 +623,7 @@ rl_status rl_scan_backward(const rl_scan_config* cfg, const void* gate, const ui
   const ScanBytes b = scan_bytes(a);
   const Span in[] = {{gate, b.gate}, {done, b.done}, {h0, b.state}, {h, b.values}, {dh, b.values}, {dh_last, b.state}};
   const Span out[] = {{du, b.values}, {dgate, b.gate}, {dh0, b.state}, {workspace, workspace_bytes}};
-  if (aliased(in, out, dh_last, dh0)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (aliased(in, out, 5, 2)) return fail(RL_EINVAL, "an output overlaps another array");
   if (!scan_aligned(a, {h, dh, du}, {h0, dh_last, dh0}, gate) || !scan_aligned(a, {}, {}, dgate))
     return fail(RL_EINVAL, "an array is not aligned to its elements");
   const size_t need = rl::scan_workspace_bytes(a, true);
@@ -682,7 +682,7 @@ rl_status rl_orthogonalize(int32_t n, int32_t rows, int32_t cols, int32_t dtype,
   const size_t es = dtype == RL_BF16 ? 2 : 4, bytes = es * (size_t)n * (size_t)rows * (size_t)cols;
   const Span in[] = {{g, bytes}};
   const Span outs[] = {{out, bytes}, {workspace, workspace_bytes}};
-  if (aliased(in, outs, g, out)) return fail(RL_EINVAL, "an output overlaps another array");
+  if (aliased(in, outs, 0, 0)) return fail(RL_EINVAL, "an output overlaps another array");
   if (!aligned_to(g, es) || !aligned_to(out, es)) return fail(RL_EINVAL, "an array is not aligned to its elements");
   const size_t need = rl::ortho_workspace_bytes(a);
   if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need))
