@@ -374,6 +374,8 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
         loss = 0.5 * ec * ec;
         dv = 0.;
       }
+    } else if (vc > 0. && off != off) {  // a NaN among the old values would be lost
+      loss = dv = off;
     }
     st[2] += loss;
   }

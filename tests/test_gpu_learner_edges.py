@@ -301,7 +301,7 @@ def test_ppo_sums_in_one_order(rows):
             assert all(torch.equal(x, y) for x, y in zip(got, want)), off
 
 
-# ---- PPO: small KL estimates ----
+# ---- PPO: small KL estimates, NaN ----
 
 
 @pytest.mark.parametrize("rows", [500, 30000])
@@ -324,3 +324,16 @@ def test_ppo_kl_of_a_close_policy(rows, delta):
     kl = float(got[2][4])
     assert kl >= 0 and abs(kl - want) <= tol, (kl, want, tol)
     _check_ppo(kw, got, False)
+
+
+@ROUTES
+def test_ppo_nan_in_old_values_is_not_hidden(rows):
+    """A NaN among the old values makes its row's value loss and gradient NaN, and no other row's."""
+    kw = _ppo(rows, 6, seed=18)
+    clean = R.ppo_loss(**_gpu_args(kw), **HYPER)
+    kw["value_old"][17] = np.nan
+    dx, dv, st = R.ppo_loss(**_gpu_args(kw), **HYPER)
+    rest = torch.arange(rows, device="cuda") != 17
+    assert torch.isnan(dv[17]) and torch.equal(dv[rest], clean[1][rest]) and torch.equal(dx, clean[0])
+    assert torch.isnan(st[0]) and torch.isnan(st[2])
+    assert torch.equal(st[[1, 3, 4, 5]], clean[2][[1, 3, 4, 5]])
