@@ -803,17 +803,17 @@ void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const
     scan_bwd_kernel<DT, DIAG, V, S, SCAN_WHOLE, GRAD><<<grid, 64 * S, 0, s>>>(p, gate, done, h0, h, dh, dh_last, du,
                                                                              dgate, dh0, ws, part, pl.seg);
   if (DIAG && GRAD)
-    scan_dlam_kernel<<<dim3((unsigned)((p.W + RED_P - 1) / RED_P), 2), RED_NT, 0, s>>>(part, (int64_t)pl.G * p.E * p.A, p.W,
-                                                               static_cast<float*>(dgate));
+    scan_dlam_kernel<<<dim3((unsigned)((p.W + RED_P - 1) / RED_P), 2), RED_NT, 0, s>>>(
+        part, (int64_t)pl.G * p.E * p.A, p.W, static_cast<float*>(dgate));
 }
 
-// One of the compiled S.
-#define RL_SCAN(DT, DIAG, V)             \
-  switch (pl.S) {                        \
-    case 1: RL_SCAN_S(DT, DIAG, V, 1); break;   \
-    case 4: RL_SCAN_S(DT, DIAG, V, 4); break;   \
-    case 8: RL_SCAN_S(DT, DIAG, V, 8); break;   \
-    default: RL_SCAN_S(DT, DIAG, V, 16); break; \
+// One of the compiled S (complex channels never take 16).
+#define RL_SCAN(DT, DIAG, V)                         \
+  switch (pl.S) {                                    \
+    case 1: RL_SCAN_S(DT, DIAG, V, 1); break;        \
+    case 4: RL_SCAN_S(DT, DIAG, V, 4); break;        \
+    case 8: RL_SCAN_S(DT, DIAG, V, 8); break;        \
+    default: RL_SCAN_S(DT, DIAG, V, DIAG ? 8 : 16);  \
   }
 
 }  // namespace
