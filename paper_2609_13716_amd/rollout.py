@@ -804,6 +804,8 @@ def orthogonalize(g, steps=5, out=None, workspace=None, stream=None):
     float32 or bfloat16); out may be g.  See rl_orthogonalize in include/rollout.h.  ``workspace``: uint8, at least
     orthogonalize_workspace_bytes(g) bytes (allocated when None)."""
     sizes = _ortho_sizes(g)
+    if abs(steps) > 0x7fffffff:
+        raise ValueError(f"steps is beyond 32 bits: {steps}")
     dev, dt, shape = _lead(g, "g"), g.dtype, g.shape
     with _on(stream, dev):
         if out is None:

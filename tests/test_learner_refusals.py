@@ -1,7 +1,8 @@
-"""Refusals of the learner's operators that come from two arguments together, before anything is launched: addresses
-that are never read."""
+"""More refusals of the learner's operators before anything is launched: through the C ABI with addresses that are never
+read, and through the binding with host tensors."""
 
 import pytest
+import torch
 
 from paper_2609_13716_amd import rollout as R
 from test_learner_abi import _at, _backward, _scan, _scan_cfg
@@ -26,3 +27,9 @@ def test_a_state_in_place_may_share_with_nothing_else(kind, dtype, steps):
         _refused(_backward(cfg, dh_last=_at(5), dh0=_at(5), **{other: _at(5)}))
     _refused(_scan(cfg, h0=_at(3), h_last=_at(3), h=_at(3)))
     _refused(_backward(cfg, dh_last=_at(5), dh0=_at(5), du=_at(5)))
+
+
+@pytest.mark.parametrize("steps", [2 ** 32 + 5, 2 ** 31, -2 ** 32 + 5])
+def test_steps_that_would_wrap(steps):
+    with pytest.raises(ValueError, match="beyond 32 bits"):
+        R.orthogonalize(torch.zeros(4, 8), steps=steps)
