@@ -337,3 +337,45 @@ def test_ppo_nan_in_old_values_is_not_hidden(rows):
     assert torch.isnan(dv[17]) and torch.equal(dv[rest], clean[1][rest]) and torch.equal(dx, clean[0])
     assert torch.isnan(st[0]) and torch.isnan(st[2])
     assert torch.equal(st[[1, 3, 4, 5]], clean[2][[1, 3, 4, 5]])
+
+
+# ---- orthogonalisation ----
+
+
+@pytest.mark.parametrize("size", [(3, 128, 192), (2, 32, 1024), (2, 512, 64)])
+def test_orthogonalize_in_one_launch_captured(size):
+    """Matrices whose one workgroup takes more than 64 KB of LDS, in a graph that is replayed with eager calls in
+    between."""
+    g, out = torch.empty(size, device="cuda"), torch.empty(size, device="cuda")
+    rng = np.random.default_rng(19)
+    fill = lambda: g.copy_(torch.from_numpy(rng.standard_normal(size).astype(np.float32)))  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    assert R.orthogonalize_workspace_bytes(g) == 0
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        R.orthogonalize(g, out=out)
+    for k in range(4):
+        fill()
+        out.fill_(float(k))
+        graph.replay()
+        got = out.clone()
+        assert torch.equal(got, R.orthogonalize(g)), k
+        err = np.linalg.norm(_np(got) - L.orthogonalize(_np(g)), axis=(1, 2))
+        m = min(size[1:])
+        assert (err <= 6 * 3.4445 ** 5 * U32 + 16 * np.sqrt(max(size[1:])) * U32 * 1.21 * np.sqrt(m)).all(), err
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_orthogonalize_large_stack_repeats_itself(dt):
+    """The largest tiles (128 x 128): every call, and every copy of a matrix in a stack, gives the same bits."""
+    g = torch.randn(1, 1024, 1024, generator=torch.Generator("cuda").manual_seed(20), device="cuda").to(dt)
+    g = g.repeat(4, 1, 1)
+    first = R.orthogonalize(g)
+    for i in range(1, 4):
+        assert torch.equal(first[i], first[0])
+    for _ in range(3):
+        assert torch.equal(R.orthogonalize(g), first)
+    want = torch.from_numpy(L.orthogonalize(_np(g[0]))).cuda()
+    size = float(want.norm())
+    tol = 6 * 3.4445 ** 5 * U32 + 16 * 32 * U32 * size + (2.0 ** -8 * size if dt == torch.bfloat16 else 0)
+    assert float((first[0].double() - want).norm()) <= tol
