@@ -23,9 +23,10 @@ namespace {
 constexpr int PPO_NT = 512;         // threads of a workgroup that does rows
 constexpr int PPO_SUM_NT = 512;     // of one that adds up advantages
 // Whether one workgroup does everything.  Its time grows with rows and actions;
-// three launches take 15.7 us whatever there is to do (rows of 6: 2000 11.6 us,
-// 3800 17.2; of 9: 2000 14.2, 2800 17.3; of 32: 1024 14.8, 1200 20.8).
-inline bool ppo_small(int64_t R, int na) { return R * (na + 8) <= 40 * 1024; }
+// three launches take 12 to 13 us in a graph, 14 to 16 called one by one,
+// whatever there is to do (one workgroup: rows of 6: 2000 12.5 us, 2900 16.5;
+// of 9: 1500 12.6, 2000 14.6; of 20: 800 11.9, 1200 14.5; of 32: 1024 15.3).
+inline bool ppo_small(int64_t R, int na) { return R * (na + 8) <= 28 * 1024; }
 constexpr int PPO_ADV_B = 64, PPO_ROW_B = 512;  // workgroups, at most (their partial sums go to the workspace)
 constexpr int PPO_STATS = 6;
 
