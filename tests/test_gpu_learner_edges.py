@@ -258,6 +258,26 @@ def test_ppo_entropy_coefficient_of_any_size(rows):
     assert (dx[torch.from_numpy(low).cuda()] == 0).all() and not bool(torch.isnan(dx).any())
 
 
+@pytest.mark.parametrize("rows,na", [(300, 6), (6000, 6), (6000, 32), (6000, 20)])
+@pytest.mark.parametrize("spread,shift", [(0.01, 0.0), (2.0, 300.0), (1.0, -1e4), (30.0, 1e6)])
+def test_ppo_borders_of_shifted_logits(rows, na, spread, shift):
+    """Ratios within a few float32 steps of a border, logits about any value and nearly equal or far apart: the side
+    (the clip fraction is exact) is float64's.  The oracle gets the logits less their row's largest, which float64 holds
+    exactly: of logits about 1e6 its log of the sum would be off by up to 2^-34 = 6e-11, and one of these ratios lies
+    1.6e-11 from its border (log r = 0.18232155926398; with the larger logits the oracle's is 0.18232155928854)."""
+    kw = _ppo(rows, na, seed=23, spread=spread)
+    kw["logits"] = (kw["logits"] + np.float32(shift)).astype(np.float32)
+    x = kw["logits"].astype(np.float64)
+    kw["actions"] = np.where(np.arange(rows) % 3 == 0, np.clip(kw["actions"], 0, na - 1), x.argmax(1)).astype(np.int32)
+    top = x.max(1, keepdims=True)
+    lp = x - top - np.log(np.exp(x - top).sum(1, keepdims=True))
+    border = np.where(np.arange(rows) % 2 == 0, 0.8, 1.2)
+    old = (lp[np.arange(rows), kw["actions"]] - np.log(border)).astype(np.float32)
+    for k in (-2, -1, 0, 1, 2):
+        kw["logp_old"] = (old + k * np.spacing(old)).astype(np.float32)
+        _check_ppo(dict(kw, logits=x - top), R.ppo_loss(**_gpu_args(kw), **HYPER), False)
+
+
 # ---- PPO: advantages ----
 
 
