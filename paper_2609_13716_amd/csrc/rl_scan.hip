@@ -163,8 +163,8 @@ constexpr int elem_bytes() { return DT == DT_F32 ? 4 : 2; }
 // its own.  This gives each XCD a run of neighbouring channels instead, so that
 // cache lines that two workgroups share (rows that are not aligned to lines)
 // are read and written once: gradients of 1001 steps x 14541 float32 channels
-// 66 us instead of 82.  One-wave workgroups gain from it where a step has 8 MB
-// and more (64 x 2.1 M complex float32: 218 us, 238 in turn); below that they
+// 73 us instead of 87.  One-wave workgroups gain from it where a step has 8 MB
+// and more (64 x 2.1 M complex float32: 428 us, 467 in turn); below that they
 // are better off in turn (128 x 262144 complex float32: 109 us, 115 in runs).
 template <int S>
 __device__ __forceinline__ int scan_block(size_t step_bytes) {
@@ -617,7 +617,8 @@ __global__ __launch_bounds__(64 * S, 4) void scan_bwd_kernel(ScanArgs a, const v
 #pragma unroll
         for (int v = 0; v < V; ++v) into[v] = carry[v];
       }
-      float fx[V], fy[V];  // this block's part of the sums over steps
+      float fx[V], fy[V];  // this block's part of the sums over steps: SCAN_K terms in float32 (at most 8 u of their
+                           // magnitudes, as the terms' own roundings), float64 from there on
 #pragma unroll
       for (int v = 0; v < V; ++v) fx[v] = fy[v] = 0.f;
 #pragma unroll
@@ -717,15 +718,16 @@ __global__ __launch_bounds__(RED_NT) void scan_dlam_kernel(const double* part, i
 // How a call is split: S waves of a workgroup over the steps, G segments.
 // Measured (one MI355X, us; float32 gates unless said otherwise):
 //   * one wave per 64 channels alone has enough bytes in flight from 2048
-//     waves on (250 steps x 131072 channels: 75 with S = 1, 92 with S = 8; at
-//     65536 channels 46 and 33);
+//     waves on (250 steps x 131072 channels: 76 with S = 1, 89 with S = 8; at
+//     65536 channels 53 and 46);
 //   * up to 256 workgroups each has a CU to itself, where 16 waves load more
-//     than 8 (2000 x 16384: 85 against 95); with more of them 8 waves leave
-//     room for a second workgroup (250 x 32768: 19 against 25).  Complex maps
-//     cost more to exchange: 8 is as good or better there at every size;
+//     than 8 (2000 x 16384: 95 against 104; complex channels, whose maps cost
+//     more to exchange, 250 x 16384: 19 against 20, gradients 32 against 33);
+//     with more of them 8 waves leave room for a second workgroup (250 x 32768:
+//     22 against 28);
 //   * segments read the inputs twice, and pay where workgroups leave most CUs
-//     idle (2000 x 4096: 31 in 8 segments, 55 in one; 2000 x 8192: 61 in 4, 71;
-//     2000 x 16384: 140 in 2, 88; 500 x 4096: 14 in 3, 17).
+//     idle (2000 x 4096: 33 in 8 segments, 67 in one; 2000 x 8192: 71 in 4, 74;
+//     2000 x 16384: 143 in 2, 90; 500 x 4096: 16 in 3, 18).
 struct ScanPlan {
   int S, G, seg;
 };
@@ -745,7 +747,7 @@ ScanPlan scan_plan(const ScanArgs& p) {
     s.seg = (int)(((p.T + g - 1) / g + block - 1) / block * block);
     s.G = (p.T + s.seg - 1) / s.seg;
   } else {
-    s.S = p.diag || waves > 256 || p.T <= block ? 8 : 16;
+    s.S = waves > 256 || p.T <= block ? 8 : 16;
   }
   return s;
 }
@@ -758,7 +760,7 @@ size_t slot_bytes(const ScanArgs& p, const ScanPlan& s) {
 // Two bfloat16 channels to a lane where rows have an even number of them and
 // every array starts at a dword.  Not for complex values: two dwords a step
 // and the wider maps leave room for too few waves (250 steps x 16384 channels:
-// 57 us with pairs, 26 without).
+// 34 us with pairs, 19 without; the gradients 75 and 26).
 bool pairs(const ScanArgs& p, std::initializer_list<const void*> values) {
   if (p.diag || p.dt != DT_BF16 || p.W % 2) return false;
   for (const void* v : values)
@@ -807,13 +809,13 @@ void run_scan_bwd(const ScanArgs& p, const ScanPlan& pl, const void* gate, const
         part, (int64_t)pl.G * p.E * p.A, p.W, static_cast<float*>(dgate));
 }
 
-// One of the compiled S (complex channels never take 16).
-#define RL_SCAN(DT, DIAG, V)                         \
-  switch (pl.S) {                                    \
-    case 1: RL_SCAN_S(DT, DIAG, V, 1); break;        \
-    case 4: RL_SCAN_S(DT, DIAG, V, 4); break;        \
-    case 8: RL_SCAN_S(DT, DIAG, V, 8); break;        \
-    default: RL_SCAN_S(DT, DIAG, V, DIAG ? 8 : 16);  \
+// One of the compiled S.
+#define RL_SCAN(DT, DIAG, V)             \
+  switch (pl.S) {                        \
+    case 1: RL_SCAN_S(DT, DIAG, V, 1); break;   \
+    case 4: RL_SCAN_S(DT, DIAG, V, 4); break;   \
+    case 8: RL_SCAN_S(DT, DIAG, V, 8); break;   \
+    default: RL_SCAN_S(DT, DIAG, V, 16); break; \
   }
 
 }  // namespace
