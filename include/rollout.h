@@ -332,7 +332,9 @@ rl_status rl_scan_backward(const rl_scan_config* cfg, const void* gate, const ui
  * whose action is illegal or outside 0..nA-1.  Rows with mask 0 give zero
  * gradients and nothing else, whatever they hold; with n = 0 everything is 0.
  * Whether r and v - v_old lie beyond their borders is decided as in
- * float64. */
+ * float64.  A ratio, or its product with adv, may pass float32's range: what
+ * fits is right and what does not is infinite, but a probability below e^-200
+ * counts as 0 and adds nothing (a logit at float32's lowest value is legal). */
 typedef struct {
   int64_t n_rows;        /* R >= 1 */
   int32_t n_actions;     /* nA in 1..32 */

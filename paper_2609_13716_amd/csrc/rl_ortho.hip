@@ -6,7 +6,8 @@
 // runs on the float16 matrix instructions with both operands split, v = hi +
 // lo / 2048 (hi the nearest float16, lo the float16 nearest to 2048 times the
 // rest), as hi hi + (hi lo + lo hi) / 2048 accumulated in float32: operands
-// keep 22 bits and what is dropped is 2^-22 of a term, at three matrix
+// keep 22 bits (from 2^-14 on; below, where float16's steps end, they are within
+// 2^-36 of the value) and what is dropped is 2^-22 of a term, at three matrix
 // instructions (a float32 matrix instruction has a sixteenth of their rate).
 // The splits' errors enter through A and B X only.  Small singular values of X
 // grow by `a` a step (485-fold in five), but B X has none of them, so what

@@ -5,10 +5,14 @@
 // busy for about as long.  A wave takes 64 consecutive rows: their 64 nA logits
 // are read as 16 nA pieces of 16 bytes and turned into one row per lane through
 // LDS (illegal actions become -inf on the way), the row stays in registers, and
-// the gradients go back the same way.  1048576 rows of 6 take 28 us, 20 of them
-// for the rows (4.0 TB/s), the rest for the two other launches.
-// Sums over rows are float64, taken in an order that depends on the sizes only:
-// per lane, wave, workgroup, then over workgroups by the launch that follows.
+// the gradients go back the same way.  1048576 rows of 6 take 30 us, 20 of them
+// for the rows (3.9 TB/s), the rest for the two other launches.
+// A row is float32, as its inputs and outputs are: the softmax, the ratio and the
+// gradients are a few float32 steps from float64's.  Log ratio, value loss and
+// sums over rows are float64, the sums taken in an order that depends on the
+// sizes only: per lane, wave, workgroup, then over workgroups by the launch that
+// follows.  Rows for which that is not enough (a ratio at a border, or beyond
+// float32) are done again by the whole wave: of usual rows one in 10000.
 //   few rows         one workgroup does everything in one launch (500 rows of
 //                    6: 7 us of GPU time; 15 in three launches);
 //   otherwise        the advantages' sums (when they are normalised or rows
@@ -456,9 +460,9 @@ __host__ __device__ constexpr int ppo_wave_bytes(int na) {
 }
 
 // Up to 20 actions the registers are held to what four waves of a SIMD may
-// have (two workgroups to a CU; at 20 that spills 8 dwords: 655361 masked rows
-// 41 us, 47 without); beyond, too much would be spilled (400000 rows of 24: 52
-// us, 42 without).
+// have (two workgroups to a CU; at 20 that spills 3 dwords: 655361 masked rows
+// 42 us, 46 without); beyond, too much would be spilled (400000 rows of 22: 41
+// us, 36 without; of 24: 55 and 38).
 template <int NA>
 __global__ __launch_bounds__(PPO_NT, NA <= 20 ? 4 : 1) void ppo_rows_kernel(PpoArgs p, PpoPart* part, int adv_blocks) {
   extern __shared__ double s_dyn[];

@@ -597,6 +597,10 @@ def gae(reward, done, value, value_last, gamma, lam, adv=None, ret=None, stream=
 
 
 # ---- a learner's operators (see the learner section of include/rollout.h) ----
+#
+# They are no autograd functions: tensors that require gradients are taken as plain values and nothing that is returned
+# has a history (scan_backward and ppo_loss return the gradients themselves).  With ``stream``, the caller keeps inputs
+# and given outputs from being freed or changed until that stream's work is done.
 
 
 def _lead(t, name):
@@ -694,8 +698,8 @@ def scan(u, gate, done=None, h0=None, h=None, h_last=None, workspace=None, strea
 
     u [T, E, A, D] with gate like u, or u [T, E, A, 2, P] with gate = lambda_bar [2, P] float32; done [T, E] uint8;
     h0 float32, one step's shape.  Returns (h, h_last): the states, and the float32 state the next call starts from
-    (h_last may be h0: the state is advanced in place).  ``workspace``: a uint8 tensor of at least
-    scan_workspace_bytes(u, gate) bytes (allocated when None)."""
+    (h_last may be h0: the state is advanced in place); autograd does not record it.  ``workspace``: a uint8 tensor of
+    at least scan_workspace_bytes(u, gate) bytes (allocated when None)."""
     z, gate_dtype, gate_shape = _scan_shapes(u, gate, "u")
     dev, dt, shape = _lead(u, "u"), u.dtype, u.shape
     state, f32 = shape[1:], torch.float32
@@ -746,8 +750,8 @@ def ppo_loss(logits, actions, logp_old, adv, value, ret, clip=0.2, value_coef=0.
 
     logits [.., nA] float32 with any leading shape (a rollout's [T, E, A]); actions int32, logp_old, adv, value, ret
     and value_old float32 and mask uint8 of that leading shape, legal uint8 like logits.  Returns (dlogits, dvalue,
-    stats), stats [6] named by PPO_STATS.  ``workspace``: uint8, at least ppo_workspace_bytes(logits) bytes
-    (allocated when None)."""
+    stats), the gradients of the loss and stats [6] named by PPO_STATS; autograd does not record it.  ``workspace``:
+    uint8, at least ppo_workspace_bytes(logits) bytes (allocated when None)."""
     dev, shape = _lead(logits, "logits"), logits.shape
     if len(shape) == 0:
         raise ValueError("logits must be [.., nA]")
@@ -801,8 +805,8 @@ def orthogonalize_workspace_bytes(g):
 
 def orthogonalize(g, steps=5, out=None, workspace=None, stream=None):
     """Newton-Schulz orthogonalisation of a weight update, or of a stack of them ([rows, cols] or [n, rows, cols],
-    float32 or bfloat16); out may be g.  See rl_orthogonalize in include/rollout.h.  ``workspace``: uint8, at least
-    orthogonalize_workspace_bytes(g) bytes (allocated when None)."""
+    float32 or bfloat16); out may be g; autograd does not record it.  See rl_orthogonalize in include/rollout.h.
+    ``workspace``: uint8, at least orthogonalize_workspace_bytes(g) bytes (allocated when None)."""
     sizes = _ortho_sizes(g)
     if abs(steps) > 0x7fffffff:
         raise ValueError(f"steps is beyond 32 bits: {steps}")

@@ -1,5 +1,5 @@
-"""The learner's operators at the ends of their inputs' ranges, against the float64 oracle: the lowest logits, ratios and
-gates beyond float32, advantages under any mask, rows at any alignment.  Tolerances as in test_gpu_learner.py unless a
+"""The learner's operators at the ends of their inputs' ranges, against the float64 oracle: the lowest logits, ratios
+and gates beyond float32, advantages under any mask, rows at any alignment.  Tolerances as in test_gpu_learner.py unless a
 test says otherwise."""
 
 import numpy as np
@@ -88,7 +88,7 @@ def test_ppo_logits_further_apart_than_float32(rows):
     low[:, 0] = False
     kw["logits"][:] = np.where(low, np.float32(-2e38), np.float32(0))
     kw["logits"][:, 0] = 2e38
-    near = dict(kw, logits=np.where(np.arange(6) == 0, np.float32(0), np.float32(-150)).repeat(rows).reshape(6, rows).T.copy())
+    near = dict(kw, logits=np.tile(np.where(np.arange(6) == 0, np.float32(0), np.float32(-150)), (rows, 1)))
     _check_far(kw, near, rows)
 
 
@@ -105,8 +105,8 @@ def test_ppo_rows_of_lowest_logits_only(rows):
 # ---- recurrence: gates of any size ----
 
 # segments; 16, 8 and 4 waves of a workgroup, pairs of bfloat16 and single channels; one wave
-GATE_SIZES = [(6400, 1, 1, 16), (900, 33, 2, 210), (900, 16, 3, 211), (300, 28, 2, 512), (300, 150, 2, 256), (48, 500, 2, 256), (32, 3, 1, 5),
-              (16, 3, 1, 5)]
+GATE_SIZES = [(6400, 1, 1, 16), (900, 33, 2, 210), (900, 16, 3, 211), (300, 28, 2, 512), (300, 150, 2, 256),
+              (48, 500, 2, 256), (32, 3, 1, 5), (16, 3, 1, 5)]
 
 
 def _forward_and_back(s):
@@ -242,7 +242,7 @@ def test_ppo_ratios_beyond_float64(rows):
     kw["actions"][:] = 1
     kw["logits"][:, 4] = LOWEST
     kw["logp_old"][:] = -1000
-    kw["adv"] = np.where(np.arange(rows) % 3 == 0, -1.0, np.where(np.arange(rows) % 3 == 1, 0.0, 1.0)).astype(np.float32)
+    kw["adv"] = (np.arange(rows) % 3 - 1).astype(np.float32)
     dx, dv, st = (_np(t) for t in R.ppo_loss(**_gpu_args(kw), **HYPER))
     assert not np.isnan(dx).any() and (dx[:, 4] == 0).all()
     assert np.isposinf(dx[::3, 1]).all() and np.isfinite(dx[1::3]).all() and np.isfinite(dx[2::3]).all()
