@@ -357,9 +357,9 @@ __device__ __forceinline__ void ppo_rows(const PpoArgs& p, const PpoNorm& nm, in
     // the smaller surrogate is the plain one unless the ratio has left the range on the advantage's side
     const bool plain = adv > 0.f ? !above : adv < 0.f ? !below : true;
     // Near a border the float32 ratio does not say on which side it lies: for u = 2^-24 the sum is off by at most 50 u
-    // (a term by u z + 6 u, z exp(-z) <= 0.37; 31 additions), its logarithm by as much and 4 u, the difference by
-    // u |log r| <= 88 u more, the exponential by 6 u and the border by u: 150 u.  The ratio may also be infinite, or
-    // make such a product, where float64's does not.
+    // (a term by u z + 6 u, z exp(-z) <= 0.37; 31 additions), its logarithm by as much and 8 u, the difference by
+    // u |log r| <= 88 u more, the exponential by 6 u and the border by u: 153 u, less than tol.  The ratio may also be
+    // infinite, or make such a product, where float64's does not.
     const float tol = 1e-5f * ratio, product = ratio * adv;
     rare = fminf(fabsf(ratio - lo), fabsf(ratio - hi)) <= tol || !(fabsf(product) <= 1e30f);
     if (!rare) {
